@@ -471,6 +471,78 @@ int dyspec_compact_kv_paged(void* k_cache, void* v_cache, const int64_t* tree_ro
                             const int32_t* n_accepted, int n_req, int max_out, int n_kv_heads, int head_dim,
                             int keep_root, int32_t* new_prefix_len, int32_t* status, dyspec_stream_t stream);
 
+/*
+ * (9) New tokens into the paged cache (the paper takes a filled cache for granted; this is the layout of (8)), with the
+ * rotary position embedding applied on the way.  Row i of k_new / v_new (and q) is a new token; request r owns rows
+ * token_offsets[r] .. token_offsets[r + 1] - 1, and its j-th new token is
+ *   - token context_len[r] + j of the paged sequence (tree_row_offset == NULL), or the pool row tree_row_offset[r] + j
+ *     (the tree rows of a plan whose tree lies apart from the pages), and
+ *   - at position context_len[r] + j, or context_len[r] + depths[row] when depths is given: the position of a draft
+ *     tree's node, as the mask builder writes them (what verification keeps of a path then has the positions of
+ *     the tokens that it becomes).
+ * Its K row and its Q row are rotated by the position's row of rope_table and rounded once to bf16; V is copied.
+ *   k_new, v_new     dev bf16, a row of n_kv_heads * head_dim values per token; k_stride, v_stride values from one row to the
+ *                    next (0 = packed), e.g. columns of one fused projection
+ *   q, q_out         dev bf16, rows of n_q_heads * head_dim, with strides of their own; q_out may be q itself (same
+ *                    stride), else it overlaps nothing.  n_q_heads = 0: K and V alone, q and q_out NULL
+ *   k_cache, v_cache dev bf16 [kv_total_rows][n_kv_heads][head_dim] (written)
+ *   token_offsets    dev int32 [n_req + 1], from 0, not decreasing;  context_len dev int32 [n_req]
+ *   n_tokens         rows of the inputs (host).  Rows from token_offsets[n_req] on belong to nobody and are left alone.
+ *   depths           dev int32 [n_tokens] or NULL;  tree_row_offset dev int64 [n_req] or NULL
+ *   page_table       dev int32 [n_req][pages_per_req]; page_size a power of two (any).  Not read with tree_row_offset
+ *                    (NULL is fine then); else it holds a page for every new token.
+ *   rope_table       dev float [n_positions][rotary_dim], 16-byte aligned: cosines of the rotary_dim / 2 angles, then
+ *                    their sines.  rotary_dim: a multiple of 16, at most head_dim (the columns behind it are copied);
+ *                    0 = no rotation, rope_table NULL
+ *   interleaved      0: value i pairs with value i + rotary_dim / 2; else value 2 i with value 2 i + 1
+ *   head_dim         64 or 128.  All bf16 pointers 16-byte aligned, strides multiples of 8.
+ *   status           dev int32 [1] or NULL: DYSPEC_ERR_INVALID_ARG when a token has no page, a row outside the pool or a
+ *                    position outside the table; nothing of such a token is written, the others are.
+ * Two new tokens with the same pool row are the caller's mistake (either may win).
+ */
+int dyspec_append_kv_paged(const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride, const void* q,
+                           int64_t q_stride, void* q_out, int64_t q_out_stride, int n_q_heads, void* k_cache, void* v_cache,
+                           int64_t kv_total_rows, const int32_t* token_offsets, const int32_t* context_len,
+                           const int32_t* depths, const int64_t* tree_row_offset, int n_req, int n_tokens,
+                           const int32_t* page_table, int pages_per_req, int page_size, const float* rope_table,
+                           int n_positions, int rotary_dim, int interleaved, int n_kv_heads, int head_dim, int32_t* status,
+                           dyspec_stream_t stream);
+
+/*
+ * (10) Causal attention of new tokens: what a step computes for requests that bring no tree (a prompt, a chunk of one, the single
+ * token of a plain decoding step).  For token i of request r's n_r new tokens, head h, context c_r:
+ *     out[i,h,:] = softmax_t(scale * <q[i,h,:], k[t,h/g,:]>) . v[t,h/g,:]   over t = 0 .. c_r + i
+ * with the types, roundings, static shapes (g, head_dim), plans, workspace rules, streams and status of (2) and (3).  Rows of the inputs
+ * and the output of request r start at n_0 + ... + n_{r-1}; a request with n_r = 0 has none.
+ *
+ * dyspec_plan_create_chunk: new tokens whose K and V are in a paged cache already, as tokens c_r .. c_r + n_r - 1 of their
+ * sequence (dyspec_append_kv_paged puts them there).
+ *   context_len  host int32 [n_req]  c_r >= 0;  n_new  host int32 [n_req]  n_r >= 0, any number, mixed at will
+ *   kv_total_rows, page_size, scale  as in dyspec_plan_create_paged
+ * dyspec_chunk_attention_paged: page_table as in dyspec_tree_attention_paged with the tree rows inside the pages (it covers
+ * c_r + n_r tokens; the same early read; a page number outside the pool reads as zeros).  Rows of a page behind the
+ * sequence's last token are not used, whatever they hold.
+ *   q    dev bf16, rows of n_q_heads * head_dim, q_stride values apart (0 = packed; a multiple of 8)
+ *   out  dev bf16 [sum n_r][n_q_heads][head_dim] (written)
+ *
+ * dyspec_plan_create_prompt, dyspec_prompt_attention: whole prompts (c_r = 0) packed one behind the other, no cache: K and V
+ * rows start at n_0 + ... + n_{r-1} too, with strides of their own (columns of one fused projection, say).
+ *
+ * Values: K and V of a sequence's own tokens must be finite.  (One that is not makes the rows behind it not finite, as the
+ * formula says; V's also rows up to 255 tokens in front of it.)  Limits: c_r + n_r, and (sum n_r) * g, below 2^31 - 256.
+ * The plans serve these calls only, and these calls take no other plans (DYSPEC_ERR_INVALID_ARG).
+ */
+int dyspec_plan_create_chunk(dyspec_plan_t** plan, int n_q_heads, int n_kv_heads, int head_dim, int n_req,
+                             const int32_t* context_len, const int32_t* n_new, int64_t kv_total_rows, int page_size, float scale);
+int dyspec_chunk_attention_paged(const dyspec_plan_t* plan, const void* q, int64_t q_stride, const void* k_cache,
+                                 const void* v_cache, const int32_t* page_table, int pages_per_req, void* out,
+                                 void* workspace, size_t workspace_bytes, int32_t* status, dyspec_stream_t stream);
+int dyspec_plan_create_prompt(dyspec_plan_t** plan, int n_q_heads, int n_kv_heads, int head_dim, int n_req,
+                              const int32_t* seq_len, float scale);
+int dyspec_prompt_attention(const dyspec_plan_t* plan, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                            const void* v, int64_t v_stride, void* out, void* workspace, size_t workspace_bytes,
+                            int32_t* status, dyspec_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -57,6 +57,12 @@ SIGNATURES = {
     "dyspec_plan_create_paged": (_i32, [_c.POINTER(_vp), _i32, _i32, _i32, _i32, _vp, _vp, _vp, _i64, _i32, _i32, _f32]),
     "dyspec_tree_attention_paged": (_i32, [_vp, _vp, _vp, _vp, _vp, _i32, _vp, _vp, _vp, _vp, _sz, _vp, _vp]),
     "dyspec_compact_kv_paged": (_i32, [_vp, _vp, _vp, _vp, _i32, _i32, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _i32, _vp, _vp, _vp]),
+    "dyspec_append_kv_paged": (_i32, [_vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _i32, _vp, _vp, _i64, _vp, _vp, _vp, _vp, _i32, _i32,
+                                      _vp, _i32, _i32, _vp, _i32, _i32, _i32, _i32, _i32, _vp, _vp]),
+    "dyspec_plan_create_chunk": (_i32, [_c.POINTER(_vp), _i32, _i32, _i32, _i32, _vp, _vp, _i64, _i32, _f32]),
+    "dyspec_chunk_attention_paged": (_i32, [_vp, _vp, _i64, _vp, _vp, _vp, _i32, _vp, _vp, _sz, _vp, _vp]),
+    "dyspec_plan_create_prompt": (_i32, [_c.POINTER(_vp), _i32, _i32, _i32, _i32, _vp, _f32]),
+    "dyspec_prompt_attention": (_i32, [_vp, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _sz, _vp, _vp]),
     "dyspec_release_cache": (_i32, []),
     "dyspec_tree_attention_static": (_i32, [_vp, _vp, _vp, _i32, _vp, _i32, _vp, _i32, _i32, _i32, _i32, _f32, _vp, _vp]),
 }
@@ -151,6 +157,13 @@ class Plan:
         self.page_size = int(page_size or 0)
         self.words_per_row = words_per_row
         self.total_nodes = int(sum(int(x) for x in n_nodes))
+
+    @classmethod
+    def _owning(cls, handle, page_size: int, total_nodes: int) -> "Plan":
+        """A plan of causal attention (dyspec_plan_create_chunk, dyspec_plan_create_prompt) around its handle."""
+        plan = cls.__new__(cls)
+        plan.handle, plan.page_size, plan.words_per_row, plan.total_nodes = handle, page_size, 0, total_nodes
+        return plan
 
     def workspace_bytes(self) -> int:
         return int(lib.dyspec_plan_workspace_bytes(self.handle))
@@ -375,6 +388,60 @@ def dyspec_compact_kv_paged(k_cache, v_cache, tree_row_offset, page_table, pages
                                        int(pages_per_req), int(page_size), _ptr(prefix_len), _ptr(accepted_nodes),
                                        _ptr(n_accepted), n_req, max_out, n_kv_heads, head_dim, int(bool(keep_root)),
                                        _ptr(new_prefix_len), _ptr(status), _stream(stream)), "dyspec_compact_kv_paged")
+
+
+def _host_i32(values: Sequence[int]):
+    return (_c.c_int32 * max(1, len(values)))(*[int(x) for x in values])
+
+
+def dyspec_plan_create_chunk(n_q_heads: int, n_kv_heads: int, head_dim: int, context_len: Sequence[int], n_new: Sequence[int],
+                             kv_total_rows: int, page_size: int, scale: float = 0.0) -> Plan:
+    """Plan of causal attention of new tokens over a paged cache (see include/dyspec.h); lengths are host sequences."""
+    if len(context_len) != len(n_new):
+        raise DyspecError(-1, "dyspec_plan_create_chunk")
+    handle = _vp()
+    _check(lib.dyspec_plan_create_chunk(_c.byref(handle), n_q_heads, n_kv_heads, head_dim, len(n_new),
+                                        _c.cast(_host_i32(context_len), _vp), _c.cast(_host_i32(n_new), _vp),
+                                        int(kv_total_rows), int(page_size), float(scale)), "dyspec_plan_create_chunk")
+    return Plan._owning(handle, int(page_size), sum(int(x) for x in n_new))
+
+
+def dyspec_chunk_attention_paged(plan: Plan, q, k_cache, v_cache, page_table, pages_per_req: int, out, workspace=None,
+                                 status=None, stream=None, q_stride: int = 0) -> None:
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(lib.dyspec_chunk_attention_paged(plan.handle, _ptr(q), q_stride, _ptr(k_cache), _ptr(v_cache), _ptr(page_table),
+                                            int(pages_per_req), _ptr(out), _ptr(workspace), ws_bytes, _ptr(status),
+                                            _stream(stream)), "dyspec_chunk_attention_paged")
+
+
+def dyspec_plan_create_prompt(n_q_heads: int, n_kv_heads: int, head_dim: int, seq_len: Sequence[int], scale: float = 0.0) -> Plan:
+    """Plan of causal attention over packed whole prompts (see include/dyspec.h); seq_len is a host sequence."""
+    handle = _vp()
+    _check(lib.dyspec_plan_create_prompt(_c.byref(handle), n_q_heads, n_kv_heads, head_dim, len(seq_len),
+                                         _c.cast(_host_i32(seq_len), _vp), float(scale)), "dyspec_plan_create_prompt")
+    return Plan._owning(handle, 0, sum(int(x) for x in seq_len))
+
+
+def dyspec_prompt_attention(plan: Plan, q, k, v, out, workspace=None, status=None, stream=None, q_stride: int = 0,
+                            k_stride: int = 0, v_stride: int = 0) -> None:
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(lib.dyspec_prompt_attention(plan.handle, _ptr(q), q_stride, _ptr(k), k_stride, _ptr(v), v_stride, _ptr(out),
+                                       _ptr(workspace), ws_bytes, _ptr(status), _stream(stream)), "dyspec_prompt_attention")
+
+
+def dyspec_append_kv_paged(k_new, v_new, q, q_out, k_cache, v_cache, kv_total_rows: int, token_offsets, context_len, depths,
+                           tree_row_offset, page_table, pages_per_req: int, page_size: int, rope_table, n_positions: int,
+                           rotary_dim: int, interleaved: bool, n_tokens: int, n_req: int, n_q_heads: int, n_kv_heads: int,
+                           head_dim: int, k_stride: int = 0, v_stride: int = 0, q_stride: int = 0, q_out_stride: int = 0,
+                           status=None, stream=None) -> None:
+    """New tokens' K and V into the paged cache, K and Q rotated by position (see include/dyspec.h).  Strides count
+    values from one token's row to the next, 0 = packed; depths and tree_row_offset may be None."""
+    _check(lib.dyspec_append_kv_paged(_ptr(k_new), k_stride, _ptr(v_new), v_stride, _ptr(q), q_stride, _ptr(q_out), q_out_stride,
+                                      n_q_heads, _ptr(k_cache), _ptr(v_cache), int(kv_total_rows), _ptr(token_offsets),
+                                      _ptr(context_len), _ptr(depths), _ptr(tree_row_offset), n_req, n_tokens,
+                                      _ptr(page_table), int(pages_per_req), int(page_size), _ptr(rope_table), n_positions,
+                                      rotary_dim, int(bool(interleaved)), n_kv_heads, head_dim, _ptr(status),
+                                      _stream(stream)), "dyspec_append_kv_paged")
 
 
 def dyspec_release_cache() -> None:

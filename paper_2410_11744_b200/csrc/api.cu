@@ -5,6 +5,7 @@
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
+#include <functional>
 #include <map>
 #include <mutex>
 #include <new>
@@ -46,8 +47,17 @@ cudaError_t launch_compact_kv_paged(void* k_cache, void* v_cache, const int64_t*
 cudaError_t launch_compact_kv(void* k_cache, void* v_cache, const int64_t* kv_row_offset, const int32_t* prefix_len,
                               const int32_t* accepted_nodes, const int32_t* n_accepted, int n_req, int max_out,
                               int row_bytes, int keep_root, int32_t* new_prefix_len, cudaStream_t stream);
+cudaError_t launch_append_kv_paged(const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride, const void* q,
+                                   int64_t q_stride, void* q_out, int64_t q_out_stride, int n_q_heads, void* k_cache,
+                                   void* v_cache, int64_t cache_rows, const int32_t* token_offsets,
+                                   const int32_t* context_len, const int32_t* depths, const int64_t* tree_row_offset,
+                                   int n_req, int n_tokens, const int32_t* page_table, int pages_per_req, int page_shift,
+                                   const float* rope_table, int n_positions, int rotary_dim, int interleaved,
+                                   int n_kv_heads, int head_dim, int32_t* status, cudaStream_t stream);
 cudaError_t launch_attn_small(int head_dim, int n_ctas, const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv,
                             const AttnParams& p, const WorkItem* host_items, bool early_start, cudaStream_t stream);
+cudaError_t launch_attn_causal(int head_dim, int n_ctas, const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv,
+                               const AttnParams& p, const WorkItem* host_items, cudaStream_t stream);
 cudaError_t launch_combine(int head_dim, int bm, int n_split_groups, const AttnParams& p, cudaStream_t stream);
 int attn_tc_max_clusters(int head_dim, int cluster_size);
 int attn_small_max_clusters(int head_dim, int cluster_size);
@@ -111,13 +121,14 @@ EncodeTiledFn get_encode_fn() {
   return fn;
 }
 
-// bf16 tensor [rows][heads][D] viewed as (D, heads, rows); box = (64, box_heads, box_rows), 128-byte swizzle.
-bool encode_map(CUtensorMap* map, const void* base, int64_t rows, int heads, int D, int box_heads, int box_rows) {
+// bf16 tensor [rows][heads][D] viewed as (D, heads, rows), rows `row_stride` values apart (0: packed); box = (64, box_heads,
+// box_rows), 128-byte swizzle.
+bool encode_map(CUtensorMap* map, const void* base, int64_t rows, int heads, int D, int box_heads, int box_rows, int64_t row_stride = 0) {
   EncodeTiledFn fn = get_encode_fn();
   if (!fn) return false;
   if (rows <= 0) rows = 1;
   const cuuint64_t dims[3] = {cuuint64_t(D), cuuint64_t(heads), cuuint64_t(rows)};
-  const cuuint64_t strides[2] = {cuuint64_t(D) * 2, cuuint64_t(heads) * D * 2};
+  const cuuint64_t strides[2] = {cuuint64_t(D) * 2, cuuint64_t(row_stride > 0 ? row_stride : int64_t(heads) * D) * 2};
   const cuuint32_t box[3] = {64u, cuuint32_t(box_heads), cuuint32_t(box_rows)};
   const cuuint32_t estr[3] = {1u, 1u, 1u};
   return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr,
@@ -169,7 +180,12 @@ cudaError_t write_table(void* dst, const void* src, size_t bytes, cudaStream_t s
 
 }  // namespace
 
+// What a plan schedules: draft trees (dyspec_plan_create, dyspec_plan_create_paged), chunks of new tokens over a paged cache, or
+// whole packed prompts (causal attention, requests with prefix_len = context and n_nodes = new tokens).
+enum class PlanKind { kTree, kChunk, kPrompt };
+
 struct dyspec_plan {
+  PlanKind kind = PlanKind::kTree;
   int hq = 0, hkv = 0, d = 0, g = 1, log2g = 0, W = 0;
   float scale = 0.f;
   int n_req = 0;
@@ -617,6 +633,96 @@ void schedule(dyspec_plan& pl) {
   }
 }
 
+// Scheduler of the causal kernel (tensor-core regime of chunk and prompt plans).  The groups, (request, kv head, tile of 256
+// packed rows), differ in length -- a row sees the keys in front of it -- so CTAs take work items from one queue, longest
+// first.  Groups longer than what a CTA should take are cut into pieces of equal length, whose partials the combine
+// launch merges: how long a piece may be is the candidate with the smallest makespan of the queue.  Costs in units of one
+// key tile of both query halves (1.3 us): kOneHalf of it when 128 rows or fewer are live, kItemCost per item (Q, pipeline
+// fill, output), kPartialCost per piece (fp32 rows instead of bf16), kCombineCost for the launch behind the kernel.
+void schedule_causal(dyspec_plan& pl) {
+  constexpr double kOneHalf = 0.7, kItemCost = 2.0, kPartialCost = 1.0, kCombineCost = 3.0;
+  struct Group { int req, kvh, row0, tiles; double unit; };
+  std::vector<Group> groups;
+  pl.total_tiles = 0;
+  const int nodes_per_tile = pl.bm / pl.g;
+  for (int r = 0; r < pl.n_req; ++r) {
+    const ReqInfo& rq = pl.reqs[size_t(r)];
+    for (int64_t n0 = 0; n0 < rq.n_nodes; n0 += nodes_per_tile) {
+      const int64_t end = std::min<int64_t>(rq.n_nodes, n0 + nodes_per_tile);
+      const int tiles = int((int64_t(rq.prefix_len) + end + pl.bn - 1) / pl.bn);
+      const double unit = (end - n0) * pl.g > pl.bm / 2 ? 1.0 : kOneHalf;
+      for (int kvh = 0; kvh < pl.hkv; ++kvh) groups.push_back({r, kvh, int(n0 * pl.g), tiles, unit});
+      pl.total_tiles += int64_t(tiles) * pl.hkv;
+    }
+  }
+  pl.n_groups = int64_t(groups.size());
+  pl.items.clear(); pl.cta_begin.assign(1, 0); pl.split_groups.clear(); pl.items_queue.clear(); pl.items_strided.clear();
+  pl.n_slots = 0; pl.max_splits = 1; pl.items_stride = 1; pl.cluster = 1; pl.dynamic = false; pl.n_ctas = 0;
+  if (groups.empty()) return;
+  const int n_sms = pl.tune.force_ctas > 0 ? pl.tune.force_ctas : pl.n_sms;
+  auto pieces_of = [&](const Group& gr, int longest) { return (gr.tiles + longest - 1) / longest; };
+  // makespan of the queue, the pieces taken longest first by the CTA that is free first
+  std::vector<double> costs, heap;
+  auto makespan = [&](int longest) {
+    costs.clear();
+    bool split = false;
+    for (const Group& gr : groups) {
+      const int n = pieces_of(gr, longest);
+      split = split || n > 1;
+      for (int c = 0; c < n; ++c)
+        costs.push_back(gr.unit * double(int64_t(gr.tiles) * (c + 1) / n - int64_t(gr.tiles) * c / n) + kItemCost + (n > 1 ? kPartialCost : 0.0));
+    }
+    std::sort(costs.begin(), costs.end(), std::greater<double>());
+    heap.assign(size_t(n_sms), 0.0);                       // a heap of equal values is one
+    for (double c : costs) {
+      std::pop_heap(heap.begin(), heap.end(), std::greater<double>());
+      heap.back() += c;
+      std::push_heap(heap.begin(), heap.end(), std::greater<double>());
+    }
+    return *std::max_element(heap.begin(), heap.end()) + (split ? kCombineCost : 0.0);
+  };
+  int longest = 0;
+  for (const Group& gr : groups) longest = std::max(longest, gr.tiles);
+  if (pl.n_groups < 8 * int64_t(n_sms) && pl.tune.whole_groups != 2) {     // (with more, the queue's tail is short whatever the pieces)
+    const int whole = longest;
+    double best = makespan(whole);
+    for (int per_sm = 1; per_sm <= 4; ++per_sm) {
+      const int64_t share = (pl.total_tiles + int64_t(n_sms) * per_sm - 1) / (int64_t(n_sms) * per_sm);
+      for (int64_t len : {share, share + 1, share + share / 4 + 1}) {
+        if (len < 2 || len >= whole) continue;
+        if (const double cost = makespan(int(len)); cost < best) { best = cost; longest = int(len); }
+      }
+    }
+  }
+  for (const Group& gr : groups) {
+    const ReqInfo& rq = pl.reqs[size_t(gr.req)];
+    const int n = pieces_of(gr, longest);
+    for (int c = 0; c < n; ++c) {
+      WorkItem it{};
+      it.kv_row0 = rq.kv_row0; it.prefix_len = rq.prefix_len; it.n_nodes = rq.n_nodes; it.node0 = rq.node0;
+      it.req = gr.req; it.kv_head = gr.kvh; it.row0 = gr.row0; it.n_in_cta = 1; it.n_splits = n;
+      it.tile_begin = int(int64_t(gr.tiles) * c / n);
+      it.tile_end = int(int64_t(gr.tiles) * (c + 1) / n);
+      it.slot = n > 1 ? pl.n_slots + c : -1;
+      it.slot0 = n > 1 ? pl.n_slots : -1;
+      it.group = n > 1 ? int(pl.split_groups.size()) : 0;
+      pl.items.push_back(it);
+    }
+    if (n > 1) {
+      GroupInfo info{};
+      info.req = gr.req; info.kv_head = gr.kvh; info.row0 = gr.row0; info.slot0 = pl.n_slots; info.n_splits = n;
+      pl.split_groups.push_back(info);
+      pl.n_slots += n;
+      pl.max_splits = std::max(pl.max_splits, n);
+    }
+  }
+  std::stable_sort(pl.items.begin(), pl.items.end(),
+                   [](const WorkItem& a, const WorkItem& b) { return a.tile_end - a.tile_begin > b.tile_end - b.tile_begin; });
+  pl.n_ctas = int(std::min<int64_t>(int64_t(pl.items.size()), n_sms));
+  pl.dynamic = int64_t(pl.items.size()) > pl.n_ctas;
+  pl.items_strided = pl.items;
+}
+
 // Device memory of the plans' tables.  A serving loop makes a plan for every step, and cudaMalloc, cudaFree (which waits
 // for the whole device) and a copy on the legacy stream (which waits for the step's earlier kernels) cost it about 0.9 ms
 // of host time that nothing overlapped: a step of 8 requests took 1.3 ms instead of 0.6.  So a destroyed plan's memory rests
@@ -982,6 +1088,91 @@ int dyspec_compact_kv_paged(void* k_cache, void* v_cache, const int64_t* tree_ro
   return e == cudaSuccess ? DYSPEC_OK : cuda_failed(e, "paged compact launch");
 }
 
+// Values from one token's row to the next: 0 stands for packed rows.  False: not a stride that 16-byte accesses can walk.
+static bool row_stride(int64_t* stride, int64_t row_values) {
+  if (*stride == 0) *stride = row_values;
+  return *stride >= row_values && (*stride & 7) == 0 && *stride < (int64_t(1) << 38);   // (2^39 bytes: a tensor map's limit is 2^40)
+}
+
+int dyspec_append_kv_paged(const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride, const void* q,
+                           int64_t q_stride, void* q_out, int64_t q_out_stride, int n_q_heads, void* k_cache, void* v_cache,
+                           int64_t kv_total_rows, const int32_t* token_offsets, const int32_t* context_len,
+                           const int32_t* depths, const int64_t* tree_row_offset, int n_req, int n_tokens,
+                           const int32_t* page_table, int pages_per_req, int page_size, const float* rope_table,
+                           int n_positions, int rotary_dim, int interleaved, int n_kv_heads, int head_dim, int32_t* status,
+                           dyspec_stream_t stream) {
+  if (n_q_heads < 0 || n_kv_heads <= 0 || n_req < 0 || n_tokens < 0 || kv_total_rows < 0 || n_positions < 0 || rotary_dim < 0)
+    return DYSPEC_ERR_INVALID_ARG;
+  if (!(head_dim == 64 || head_dim == 128) || n_q_heads > (1 << 16) || n_kv_heads > (1 << 16)) return DYSPEC_ERR_UNSUPPORTED;
+  if (rotary_dim % 16 != 0) return DYSPEC_ERR_UNSUPPORTED;
+  if (rotary_dim > head_dim) return DYSPEC_ERR_INVALID_ARG;
+  if (!tree_row_offset && (pages_per_req <= 0 || page_size <= 0 || (page_size & (page_size - 1)))) return DYSPEC_ERR_INVALID_ARG;
+  const int64_t q_row = int64_t(n_q_heads) * head_dim, kv_row = int64_t(n_kv_heads) * head_dim;
+  if (!row_stride(&k_stride, kv_row) || !row_stride(&v_stride, kv_row) || !row_stride(&q_stride, q_row) || !row_stride(&q_out_stride, q_row))
+    return DYSPEC_ERR_INVALID_ARG;
+  if (n_req == 0 || n_tokens == 0) return DYSPEC_OK;
+  if (!k_new || !v_new || !k_cache || !v_cache || !token_offsets || !context_len || (!tree_row_offset && !page_table))
+    return DYSPEC_ERR_INVALID_ARG;
+  if (n_q_heads > 0 && (!q || !q_out || !aligned(q, 16) || !aligned(q_out, 16) || (q == q_out && q_stride != q_out_stride)))
+    return DYSPEC_ERR_INVALID_ARG;
+  if (rotary_dim > 0 && (!rope_table || !aligned(rope_table, 16))) return DYSPEC_ERR_INVALID_ARG;
+  if (!aligned(k_new, 16) || !aligned(v_new, 16) || !aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(token_offsets, 4) ||
+      !aligned(context_len, 4) || !aligned(depths, 4) || !aligned(tree_row_offset, 8) || !aligned(page_table, 4) || !aligned(status, 4))
+    return DYSPEC_ERR_INVALID_ARG;
+  int shift = 0;
+  while (!tree_row_offset && (int64_t(1) << shift) < page_size) ++shift;
+  cudaError_t e = launch_append_kv_paged(k_new, k_stride, v_new, v_stride, q, q_stride, q_out, q_out_stride, n_q_heads, k_cache,
+                                         v_cache, kv_total_rows, token_offsets, context_len, depths, tree_row_offset, n_req,
+                                         n_tokens, page_table, pages_per_req, shift, rope_table, n_positions, rotary_dim,
+                                         interleaved != 0, n_kv_heads, head_dim, status, reinterpret_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? DYSPEC_OK : cuda_failed(e, "append launch");
+}
+
+// The part of planning behind the checks: regime, schedule, workspace.
+static void finish_host_plan(dyspec_plan* pl, int64_t max_rows) {
+  // Regime: tcgen05 tiles (2 x 128 packed rows per item) when some request has more packed rows
+  // (nodes x group) than one warp-level tile holds, else warp-level tiles (64 packed rows).
+  pl->tune = current_tuning();
+  pl->n_sms = device_sm_count();
+  pl->regime = pl->tune.force_regime >= 0 ? pl->tune.force_regime : (max_rows > 64 ? 1 : 0);
+  pl->bm = pl->regime == 0 ? 64 : 256;    // packed query rows per work item (regime 1: two 128-row halves)
+  pl->bn = pl->regime == 0 ? 64 : 128;    // keys per tile
+  if (pl->tune.combine_mode == 2)
+    for (int C : {2, 4, 8})
+      pl->cluster_fit[C] = pl->regime == 1 ? attn_tc_max_clusters(pl->d, C) : attn_small_max_clusters(pl->d, C);
+  if (pl->kind != PlanKind::kTree && pl->regime == 1) {
+    pl->tune.combine_mode = 0;            // the causal kernel's partials are merged by the combine launch
+    schedule_causal(*pl);
+  } else {
+    schedule(*pl);
+  }
+  // A cluster plan of the tensor-core regime needs C CTAs of 1 CTA / SM side by side: where the device cannot
+  // hold even one such cluster (a reduced share of its SMs), plan again without clusters.
+  // (The same when the device cannot hold all of the plan's clusters at once -- the SMs of a cluster have to
+  //  come from one GPC -- since the clusters left over would run as a second wave.)
+  if (pl->regime == 1 && pl->cluster > 1) {
+    const int fit = attn_tc_max_clusters(pl->d, pl->cluster);
+    if (fit >= 0 && fit < pl->n_ctas / pl->cluster) {
+      pl->tune.combine_mode = 1;
+      schedule(*pl);
+    }
+  }
+  pl->workspace_bytes = size_t(pl->n_slots) * size_t(pl->bm) * (pl->d + 2) * sizeof(float);
+  if (pl->regime == 1 && pl->cluster > 1)   // cluster plan: the shares a CTA's peers cannot push into its shared memory
+    pl->workspace_bytes = size_t(pl->n_ctas) * attn_tc_cluster_workspace_per_cta(pl->d, pl->cluster);
+  if (!pl->split_groups.empty()) {      // the groups' counter pairs follow the partials
+    pl->counters_offset = (pl->workspace_bytes + 255) & ~size_t(255);
+    pl->workspace_bytes = pl->counters_offset + ((pl->split_groups.size() * 2 * sizeof(int32_t) + 255) & ~size_t(255));
+    // (the items of a group wait for each other inside the kernel: only when every CTA of the launch is
+    //  resident at once, i.e. one CTA per SM and no more CTAs than SMs; a forced larger grid keeps the combine launch)
+    pl->merge_in_kernel = pl->regime == 1 && pl->tune.combine_mode != 0 && pl->n_ctas <= pl->n_sms;
+  }
+  if (pl->dynamic) {                    // the queue words follow the partials (there are none in such a plan today)
+    pl->queue_offset = (pl->workspace_bytes + 255) & ~size_t(255);
+    pl->workspace_bytes = pl->queue_offset + 256;
+  }
+}
+
 // Validates the arguments and runs the scheduler; no CUDA call.
 static int make_host_plan(dyspec_plan** out, int n_q_heads, int n_kv_heads, int head_dim, int n_req,
                           const int32_t* prefix_len, const int32_t* n_nodes, const int64_t* kv_row_offset,
@@ -1026,42 +1217,7 @@ static int make_host_plan(dyspec_plan** out, int n_q_heads, int n_kv_heads, int 
   }
   if (node0 >= (int64_t(1) << 31)) { delete pl; return DYSPEC_ERR_UNSUPPORTED; }
   pl->total_nodes = node0;
-  // Regime: tcgen05 tiles (2 x 128 packed rows per item) when some request has more packed rows
-  // (nodes x group) than one warp-level tile holds, else warp-level tiles (64 packed rows).
-  pl->tune = current_tuning();
-  pl->n_sms = device_sm_count();
-  pl->regime = pl->tune.force_regime >= 0 ? pl->tune.force_regime : (max_rows > 64 ? 1 : 0);
-  pl->bm = pl->regime == 0 ? 64 : 256;    // packed query rows per work item (regime 1: two 128-row halves)
-  pl->bn = pl->regime == 0 ? 64 : 128;    // keys per tile
-  if (pl->tune.combine_mode == 2)
-    for (int C : {2, 4, 8})
-      pl->cluster_fit[C] = pl->regime == 1 ? attn_tc_max_clusters(pl->d, C) : attn_small_max_clusters(pl->d, C);
-  schedule(*pl);
-  // A cluster plan of the tensor-core regime needs C CTAs of 1 CTA / SM side by side: where the device cannot
-  // hold even one such cluster (a reduced share of its SMs), plan again without clusters.
-  // (The same when the device cannot hold all of the plan's clusters at once -- the SMs of a cluster have to
-  //  come from one GPC -- since the clusters left over would run as a second wave.)
-  if (pl->regime == 1 && pl->cluster > 1) {
-    const int fit = attn_tc_max_clusters(pl->d, pl->cluster);
-    if (fit >= 0 && fit < pl->n_ctas / pl->cluster) {
-      pl->tune.combine_mode = 1;
-      schedule(*pl);
-    }
-  }
-  pl->workspace_bytes = size_t(pl->n_slots) * size_t(pl->bm) * (pl->d + 2) * sizeof(float);
-  if (pl->regime == 1 && pl->cluster > 1)   // cluster plan: the shares a CTA's peers cannot push into its shared memory
-    pl->workspace_bytes = size_t(pl->n_ctas) * attn_tc_cluster_workspace_per_cta(pl->d, pl->cluster);
-  if (!pl->split_groups.empty()) {      // the groups' counter pairs follow the partials
-    pl->counters_offset = (pl->workspace_bytes + 255) & ~size_t(255);
-    pl->workspace_bytes = pl->counters_offset + ((pl->split_groups.size() * 2 * sizeof(int32_t) + 255) & ~size_t(255));
-    // (the items of a group wait for each other inside the kernel: only when every CTA of the launch is
-    //  resident at once, i.e. one CTA per SM and no more CTAs than SMs; a forced larger grid keeps the combine launch)
-    pl->merge_in_kernel = pl->regime == 1 && pl->tune.combine_mode != 0 && pl->n_ctas <= pl->n_sms;
-  }
-  if (pl->dynamic) {                    // the queue words follow the partials (there are none in such a plan today)
-    pl->queue_offset = (pl->workspace_bytes + 255) & ~size_t(255);
-    pl->workspace_bytes = pl->queue_offset + 256;
-  }
+  finish_host_plan(pl, max_rows);
   *out = pl;
   return DYSPEC_OK;
 }
@@ -1098,6 +1254,75 @@ int dyspec_plan_create_paged(dyspec_plan_t** plan, int n_q_heads, int n_kv_heads
   if (rc != DYSPEC_OK) { dyspec_plan_destroy(pl); return rc; }
   *plan = pl;
   return DYSPEC_OK;
+}
+
+// Plans of causal attention: chunks over a paged cache (page_size > 0) or packed prompts (page_size = 0, contexts NULL).
+static int make_causal_plan(dyspec_plan_t** out, PlanKind kind, int n_q_heads, int n_kv_heads, int head_dim, int n_req,
+                            const int32_t* context_len, const int32_t* n_new, int64_t kv_total_rows, int page_size, float scale) {
+  if (!out) return DYSPEC_ERR_INVALID_ARG;
+  *out = nullptr;
+  if (n_q_heads <= 0 || n_kv_heads <= 0 || n_req < 0 || kv_total_rows < 0) return DYSPEC_ERR_INVALID_ARG;
+  if (n_req > 0 && (!n_new || (kind == PlanKind::kChunk && !context_len))) return DYSPEC_ERR_INVALID_ARG;
+  if (kind == PlanKind::kChunk) {
+    if (page_size <= 0 || (page_size & (page_size - 1))) return DYSPEC_ERR_INVALID_ARG;
+    if (page_size < 128 || page_size > (1 << 20)) return DYSPEC_ERR_UNSUPPORTED;
+  }
+  if (n_q_heads % n_kv_heads != 0) return DYSPEC_ERR_UNSUPPORTED;
+  const int g = n_q_heads / n_kv_heads;
+  if (!(g == 1 || g == 2 || g == 4 || g == 8) || !(head_dim == 64 || head_dim == 128)) return DYSPEC_ERR_UNSUPPORTED;
+  if (kv_total_rows >= (int64_t(1) << 31)) return DYSPEC_ERR_UNSUPPORTED;
+  int64_t total = 0, max_rows = 0, groups = 0;
+  for (int r = 0; r < n_req; ++r) {
+    const int64_t c = kind == PlanKind::kChunk ? context_len[r] : 0, n = n_new[r];
+    if (c < 0 || n < 0) return DYSPEC_ERR_INVALID_ARG;
+    if (c + n >= (int64_t(1) << 31) - 256) return DYSPEC_ERR_UNSUPPORTED;      // (key and packed-row indices stay in 32 bits)
+    total += n;
+    max_rows = std::max(max_rows, n * g);
+    groups += ((n * g + 63) / 64) * n_kv_heads;
+  }
+  if (total * g >= (int64_t(1) << 31) - 256 || groups > (int64_t(1) << 22)) return DYSPEC_ERR_UNSUPPORTED;
+  dyspec_plan* pl = nullptr;
+  int rc = DYSPEC_OK;
+  try {
+    pl = new dyspec_plan();
+    pl->kind = kind;
+    pl->hq = n_q_heads; pl->hkv = n_kv_heads; pl->d = head_dim; pl->g = g;
+    pl->log2g = g == 1 ? 0 : g == 2 ? 1 : g == 4 ? 2 : 3;
+    pl->scale = scale > 0.f ? scale : 1.0f / std::sqrt(float(head_dim));
+    pl->n_req = n_req;
+    pl->page_size = page_size;
+    pl->tree_in_pages = true;             // key tiles follow the sequence
+    pl->kv_total_rows = kind == PlanKind::kChunk ? kv_total_rows : total;
+    pl->total_nodes = total;
+    int64_t node0 = 0;
+    for (int r = 0; r < n_req; ++r) {
+      ReqInfo rq{};
+      rq.kv_row0 = kind == PlanKind::kChunk ? 0 : node0;
+      rq.prefix_len = kind == PlanKind::kChunk ? context_len[r] : 0;
+      rq.n_nodes = n_new[r]; rq.node0 = int32_t(node0);
+      pl->reqs.push_back(rq);
+      node0 += n_new[r];
+      pl->max_nodes = std::max(pl->max_nodes, int(n_new[r]));
+    }
+    finish_host_plan(pl, max_rows);
+    rc = upload(*pl);
+  } catch (const std::bad_alloc&) {
+    rc = DYSPEC_ERR_CUDA;
+  }
+  if (rc != DYSPEC_OK) { dyspec_plan_destroy(pl); return rc; }
+  *out = pl;
+  return DYSPEC_OK;
+}
+
+int dyspec_plan_create_chunk(dyspec_plan_t** plan, int n_q_heads, int n_kv_heads, int head_dim, int n_req,
+                             const int32_t* context_len, const int32_t* n_new, int64_t kv_total_rows, int page_size, float scale) {
+  return make_causal_plan(plan, PlanKind::kChunk, n_q_heads, n_kv_heads, head_dim, n_req, context_len, n_new, kv_total_rows,
+                          page_size, scale);
+}
+
+int dyspec_plan_create_prompt(dyspec_plan_t** plan, int n_q_heads, int n_kv_heads, int head_dim, int n_req,
+                              const int32_t* seq_len, float scale) {
+  return make_causal_plan(plan, PlanKind::kPrompt, n_q_heads, n_kv_heads, head_dim, n_req, nullptr, seq_len, 0, 0, scale);
 }
 
 int dyspec_schedule_dry_run(int n_q_heads, int n_kv_heads, int head_dim, int n_req, const int32_t* prefix_len,
@@ -1161,7 +1386,7 @@ int64_t dyspec_plan_info(const dyspec_plan_t* plan, int field) {
 
 static int plan_build_tree_mask_checked(const dyspec_plan_t* plan, const int32_t* parents, uint32_t* ancestor_bits,
                                         int32_t* depths, uint32_t* node_tiles, int32_t* status, dyspec_stream_t stream) {
-  if (!plan) return DYSPEC_ERR_INVALID_ARG;
+  if (!plan || plan->kind != PlanKind::kTree) return DYSPEC_ERR_INVALID_ARG;
   if (plan->n_req == 0 || plan->total_nodes == 0) return DYSPEC_OK;
   if (!parents || !ancestor_bits || !aligned(ancestor_bits, 16) || !aligned(node_tiles, 4)) return DYSPEC_ERR_INVALID_ARG;
   cudaError_t e = launch_build_tree_mask(parents, plan->d_reqs, plan->n_req, 0, plan->max_nodes, ancestor_bits, depths,
@@ -1182,7 +1407,7 @@ int dyspec_plan_build_tree_mask_tiles(const dyspec_plan_t* plan, const int32_t* 
 
 int dyspec_plan_dfs_reorder(const dyspec_plan_t* plan, const int32_t* parents, int32_t* order, int32_t* new_of_old,
                             int32_t* new_parents, int32_t* status, dyspec_stream_t stream) {
-  if (!plan) return DYSPEC_ERR_INVALID_ARG;
+  if (!plan || plan->kind != PlanKind::kTree) return DYSPEC_ERR_INVALID_ARG;
   if (plan->n_req == 0 || plan->total_nodes == 0) return DYSPEC_OK;
   if (!parents || !aligned(parents, 4) || !aligned(order, 4) || !aligned(new_of_old, 4) || !aligned(new_parents, 4))
     return DYSPEC_ERR_INVALID_ARG;
@@ -1207,13 +1432,18 @@ static bool list_read_early(const dyspec_plan& pl) { return pl.items_stride > 1 
 static int run_attention(const dyspec_plan_t* plan, const void* q, const void* k_cache, const void* v_cache,
                          const int32_t* page_table, int pages_per_req, const uint32_t* ancestor_bits,
                          const uint32_t* node_tiles, void* out, void* workspace, size_t workspace_bytes, int32_t* status,
-                         dyspec_stream_t stream, bool tables_in_stream = false);
+                         dyspec_stream_t stream, bool tables_in_stream = false, int64_t q_stride = 0, int64_t k_stride = 0,
+                         int64_t v_stride = 0);
+static int paged_attention(const dyspec_plan_t* plan, const void* q, int64_t q_stride, const void* k_cache, const void* v_cache,
+                           const int32_t* page_table, int pages_per_req, const uint32_t* ancestor_bits,
+                           const uint32_t* node_tiles, void* out, void* workspace, size_t workspace_bytes, int32_t* status,
+                           dyspec_stream_t stream);
 
 int dyspec_tree_attention_ragged_sparse(const dyspec_plan_t* plan, const void* q, const void* k_cache,
                                         const void* v_cache, const uint32_t* ancestor_bits, const uint32_t* node_tiles,
                                         void* out, void* workspace, size_t workspace_bytes, int32_t* status,
                                         dyspec_stream_t stream) {
-  if (plan && plan->page_size != 0) return DYSPEC_ERR_INVALID_ARG;      // a paged plan needs its page table
+  if (plan && (plan->page_size != 0 || plan->kind != PlanKind::kTree)) return DYSPEC_ERR_INVALID_ARG;   // a paged plan needs its page table
   return run_attention(plan, q, k_cache, v_cache, nullptr, 0, ancestor_bits, node_tiles, out, workspace, workspace_bytes,
                        status, stream);
 }
@@ -1222,24 +1452,53 @@ int dyspec_tree_attention_paged(const dyspec_plan_t* plan, const void* q, const 
                                 const int32_t* page_table, int pages_per_req, const uint32_t* ancestor_bits,
                                 const uint32_t* node_tiles, void* out, void* workspace, size_t workspace_bytes,
                                 int32_t* status, dyspec_stream_t stream) {
-  if (!plan || plan->page_size == 0) return DYSPEC_ERR_INVALID_ARG;
+  if (!plan || plan->page_size == 0 || plan->kind != PlanKind::kTree) return DYSPEC_ERR_INVALID_ARG;
+  return paged_attention(plan, q, 0, k_cache, v_cache, page_table, pages_per_req, ancestor_bits, node_tiles, out, workspace,
+                         workspace_bytes, status, stream);
+}
+
+int dyspec_chunk_attention_paged(const dyspec_plan_t* plan, const void* q, int64_t q_stride, const void* k_cache,
+                                 const void* v_cache, const int32_t* page_table, int pages_per_req, void* out,
+                                 void* workspace, size_t workspace_bytes, int32_t* status, dyspec_stream_t stream) {
+  if (!plan || plan->kind != PlanKind::kChunk || !row_stride(&q_stride, int64_t(plan->hq) * plan->d)) return DYSPEC_ERR_INVALID_ARG;
+  return paged_attention(plan, q, q_stride, k_cache, v_cache, page_table, pages_per_req, nullptr, nullptr, out, workspace,
+                         workspace_bytes, status, stream);
+}
+
+int dyspec_prompt_attention(const dyspec_plan_t* plan, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                            const void* v, int64_t v_stride, void* out, void* workspace, size_t workspace_bytes,
+                            int32_t* status, dyspec_stream_t stream) {
+  if (!plan || plan->kind != PlanKind::kPrompt) return DYSPEC_ERR_INVALID_ARG;
+  const int64_t kv_row = int64_t(plan->hkv) * plan->d;
+  if (!row_stride(&q_stride, int64_t(plan->hq) * plan->d) || !row_stride(&k_stride, kv_row) || !row_stride(&v_stride, kv_row))
+    return DYSPEC_ERR_INVALID_ARG;
+  return run_attention(plan, q, k, v, nullptr, 0, nullptr, nullptr, out, workspace, workspace_bytes, status, stream, false,
+                       q_stride, k_stride, v_stride);
+}
+
+// The paged calls behind the check of the plan's kind.
+static int paged_attention(const dyspec_plan_t* plan, const void* q, int64_t q_stride, const void* k_cache, const void* v_cache,
+                           const int32_t* page_table, int pages_per_req, const uint32_t* ancestor_bits,
+                           const uint32_t* node_tiles, void* out, void* workspace, size_t workspace_bytes, int32_t* status,
+                           dyspec_stream_t stream) {
   if (plan->n_ctas == 0) return DYSPEC_OK;
   if (!page_table || !aligned(page_table, 4) || pages_per_req <= 0) return DYSPEC_ERR_INVALID_ARG;
   for (const ReqInfo& rq : plan->reqs)                                   // every prefix token has a table entry
     if ((int64_t(rq.prefix_len) + (plan->tree_in_pages ? rq.n_nodes : 0) + plan->page_size - 1) / plan->page_size > pages_per_req)
       return DYSPEC_ERR_INVALID_ARG;
   return run_attention(plan, q, k_cache, v_cache, page_table, pages_per_req, ancestor_bits, node_tiles, out, workspace,
-                       workspace_bytes, status, stream);
+                       workspace_bytes, status, stream, false, q_stride);
 }
 
 static int run_attention(const dyspec_plan_t* plan, const void* q, const void* k_cache, const void* v_cache,
                          const int32_t* page_table, int pages_per_req, const uint32_t* ancestor_bits,
                          const uint32_t* node_tiles, void* out, void* workspace, size_t workspace_bytes, int32_t* status,
-                         dyspec_stream_t stream, bool tables_in_stream) {
+                         dyspec_stream_t stream, bool tables_in_stream, int64_t q_stride, int64_t k_stride, int64_t v_stride) {
   if (!plan) return DYSPEC_ERR_INVALID_ARG;
+  const bool causal = plan->kind != PlanKind::kTree;       // no mask to read
   if (!aligned(node_tiles, 4)) return DYSPEC_ERR_INVALID_ARG;
   if (plan->n_ctas == 0) return DYSPEC_OK;
-  if (!q || !k_cache || !v_cache || !ancestor_bits || !out) return DYSPEC_ERR_INVALID_ARG;
+  if (!q || !k_cache || !v_cache || (!ancestor_bits && !causal) || !out) return DYSPEC_ERR_INVALID_ARG;
   if (!aligned(q, 16) || !aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(out, 16) || !aligned(ancestor_bits, 16))
     return DYSPEC_ERR_INVALID_ARG;
   int dev = -1;                          // the plan's tables live on the device it was created on
@@ -1252,12 +1511,14 @@ static int run_attention(const dyspec_plan_t* plan, const void* q, const void* k
   CUtensorMap mq, mk, mv;
   const int bm = plan->bm, bn = plan->bn;
   const int q_box_rows = plan->regime == 0 ? 64 : 128;   // packed rows per TMA box of Q
-  if (!encode_map(&mq, q, plan->total_nodes, plan->hq, plan->d, plan->g, q_box_rows / plan->g) ||
-      !encode_map(&mk, k_cache, plan->kv_total_rows, plan->hkv, plan->d, 1, bn) ||
-      !encode_map(&mv, v_cache, plan->kv_total_rows, plan->hkv, plan->d, 1, bn))
+  if (!encode_map(&mq, q, plan->total_nodes, plan->hq, plan->d, plan->g, q_box_rows / plan->g, q_stride) ||
+      !encode_map(&mk, k_cache, plan->kv_total_rows, plan->hkv, plan->d, 1, bn, k_stride) ||
+      !encode_map(&mv, v_cache, plan->kv_total_rows, plan->hkv, plan->d, 1, bn, v_stride))
     return DYSPEC_ERR_CUDA;
 
   AttnParams p{};
+  p.causal = causal ? 1 : 0;
+  p.kv_total_rows = plan->kv_total_rows;
   p.reqs = plan->d_reqs; p.items = plan->d_items; p.groups = plan->d_groups;
   p.bits = ancestor_bits; p.out = static_cast<__nv_bfloat16*>(out);
   p.node_tiles = plan->tree_in_pages ? nullptr : node_tiles;   // the tile sets count unshifted tree tiles
@@ -1284,6 +1545,7 @@ static int run_attention(const dyspec_plan_t* plan, const void* q, const void* k
   cudaError_t e;
   const bool early = !tables_in_stream || !list_read_early(*plan);
   if (plan->regime == 0) e = launch_attn_small(plan->d, plan->n_ctas, mq, mk, mv, p, plan->items_strided.data(), early, st);
+  else if (causal) e = launch_attn_causal(plan->d, plan->n_ctas, mq, mk, mv, p, plan->items_strided.data(), st);
   else e = launch_attn_tc(plan->d, plan->n_ctas, mq, mk, mv, p, plan->items_strided.data(), early, st);
   if (e != cudaSuccess) return cuda_failed(e, "attention launch");
   if (plan->merge_in_kernel) return DYSPEC_OK;

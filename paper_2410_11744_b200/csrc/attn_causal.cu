@@ -1,0 +1,505 @@
+// Causal attention of new tokens (a chunk of a sequence over its paged cache, or whole packed prompts), for requests whose
+// packed rows (tokens x GQA group) fill 128-row tiles:
+//   out_i = sum_{t <= c + i} softmax_t(scale <q_i, k_t>) v_t          (token i of the chunk is token c + i of its sequence)
+//
+// One CTA per SM, 12 warps; a work item is 256 packed query rows of one (request, kv head), two halves A and B of 128, against
+// a range of 128-key tiles:
+//   warp 0       TMA producer: the item's Q (half A, then B), then K and V tiles into a shared-memory ring;
+//   warps 1, 3   tcgen05.mma issuers of half A / B: S = Q K^T (both operands in shared memory), O += P V (P in tensor memory);
+//   warp 2       tensor memory: S_A, S_B (128 fp32 columns each), O_A, O_B (D each);
+//   warps 4-7    softmax of half A, a row per thread: fp32 online softmax in the exp2 domain; warps 8-11 of half B.
+// A half's P (bf16) takes the place of its S: a thread has its row of scores in registers before it writes the first
+// probability.  Products of one issuing thread run in order, so S(j + 1), issued behind P V(j), overwrites a P that has
+// been read, and "S(j + 1) is there" also says that P V(j) is done: one barrier tells the softmax threads both, and the
+// running output may be rescaled then without another wait.  The tensor pipe works for the other half meanwhile.
+// P is handed over in two pieces of 64 keys, so that the first half of P V runs under the second half of the exponentials.
+//
+// CTAs take items from a queue, longest first (see schedule_causal in api.cu); an item whose group was cut along the
+// keys writes an fp32 partial (O, m, l) that combine_kernel merges.  Every wait on an mbarrier is bounded (see mbar_wait).
+#include "tc_ops.cuh"
+
+namespace dyspec {
+
+namespace {
+
+constexpr int BMH = 128;          // rows of one query half
+constexpr int BN = 128;           // keys per tile
+constexpr int kThreads = 384;
+constexpr uint32_t kTmemCols = 512;
+constexpr float kRescaleThreshold = 8.0f;   // log2 units: the output is rescaled only when a row maximum grows by more
+
+template <int D>
+struct CausalLayout {
+  static constexpr int kSlots = D == 128 ? 5 : 10;            // K / V tiles in the ring
+  static constexpr int kPanels = D / 64;
+  static constexpr int kPanelBytes = 128 * 128;               // 128 rows x 128 bytes
+  static constexpr int kTileBytes = kPanels * kPanelBytes;    // one K tile, V tile or query half
+  static constexpr int kRingOffset = 2 * kTileBytes;
+  static constexpr int kBarOffset = kRingOffset + kSlots * kTileBytes;
+  static constexpr int kItemRingOffset = kBarOffset + 512;    // the CTA's next work items, 8 entries of 64 bytes
+  static constexpr int kTotal = kItemRingOffset + 512;
+};
+
+// mbarriers (8 bytes each), behind them: tensor-memory address, abort flag, indexes of the item ring
+template <int kSlots>
+struct Bars {
+  static constexpr int kQFull = 0;                      // [2] query half A / B is in shared memory
+  static constexpr int kQFree = 2;                      // both halves' last S products have run
+  static constexpr int kSlotFull = 3;                   // [kSlots]
+  static constexpr int kSlotEmpty = kSlotFull + kSlots; // [kSlots] two commits, one per half
+  static constexpr int kSReady = kSlotEmpty + kSlots;   // [2]
+  static constexpr int kODone = kSReady + 2;            // [2] the item's last P V has run
+  static constexpr int kOFree = kODone + 2;             // [2] the output has been read out
+  static constexpr int kItemFull = kOFree + 2;          // [8] item ring entry written
+  static constexpr int kItemEmpty = kItemFull + 8;      // [8] ... and read by the issuing and softmax warps
+  static constexpr int kCount = kItemEmpty + 8;
+};
+
+constexpr int kBarP = 1;                    // named barriers 1 .. 4: 64 keys of P are in tensor memory (half A: 1, 2; half B: 3, 4)
+constexpr int kPCount = BMH + 32;           // a half's softmax threads + the issuing warp
+
+}  // namespace
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1)
+causal_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                   const __grid_constant__ CUtensorMap map_v, const AttnParams p, const __grid_constant__ FirstItems first) {
+  using L = CausalLayout<D>;
+  constexpr int kSlots = L::kSlots;
+  using Br = Bars<kSlots>;
+  static_assert(8 * Br::kCount + 48 <= 512, "barrier area");
+  extern __shared__ __align__(1024) uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  const uint32_t s_q = smem_u32(smem);
+  const uint32_t s_ring = s_q + L::kRingOffset;
+  const uint32_t s_bar = s_q + L::kBarOffset;
+  auto bar = [&](int i) { return s_bar + 8u * uint32_t(i); };
+  volatile uint32_t* tmem_holder = reinterpret_cast<volatile uint32_t*>(smem + L::kBarOffset + 8 * Br::kCount);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + L::kBarOffset + 8 * Br::kCount + 8);
+  volatile int32_t* ring_idx = reinterpret_cast<volatile int32_t*>(smem + L::kBarOffset + 8 * Br::kCount + 16);
+  uint4* ring_item = reinterpret_cast<uint4*>(smem + L::kItemRingOffset);
+
+  const int warp = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31;
+  if (threadIdx.x == 0) {
+    for (int h = 0; h < 2; ++h) {
+      mbar_init(bar(Br::kQFull + h), 1);
+      mbar_init(bar(Br::kSReady + h), 1);
+      mbar_init(bar(Br::kODone + h), 1);
+      mbar_init(bar(Br::kOFree + h), BMH);
+    }
+    mbar_init(bar(Br::kQFree), 2);
+    for (int s = 0; s < kSlots; ++s) {
+      mbar_init(bar(Br::kSlotFull + s), 1);
+      mbar_init(bar(Br::kSlotEmpty + s), 2);
+    }
+    for (int e = 0; e < 8; ++e) {
+      mbar_init(bar(Br::kItemFull + e), 1);
+      mbar_init(bar(Br::kItemEmpty + e), 2 + 2 * BMH / 32);
+    }
+    *abort_flag = 0;
+    fence_barrier_init();
+  }
+  if (warp == 2) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
+                 ::"r"(smem_u32(const_cast<uint32_t*>(tmem_holder))), "r"(kTmemCols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_holder;
+
+  // The CTA's first item is item blockIdx.x of the queue and travels with the kernel parameters; the producer warp takes
+  // further ones with an atomic add and passes them on through a ring of 8 entries.  No queue (p.queue null): one item per CTA.
+  const bool first_here = blockIdx.x < kFirstItems;
+  auto item_of = [&](int w, bool consumer = true) -> WorkItem {
+    if (w == 0) return first_here ? first.item[blockIdx.x] : p.items[blockIdx.x];
+    union { WorkItem it; uint4 v[4]; } u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u.v[i] = ring_item[((w - 1) & 7) * 4 + i];
+    if (consumer) {
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar(Br::kItemEmpty + ((w - 1) & 7)));
+    }
+    return u.it;
+  };
+  auto take_item = [&](int w) -> bool {                    // producer warp, all lanes
+    if (w == 0) return true;
+    if (p.queue == nullptr) return false;
+    int idx = 0;
+    if (lane == 0) {
+      if (w == 1) grid_dependency_wait();                  // the last launch on this workspace cleared the queue words
+      const int t = atomicAdd(p.queue, 1) + int(gridDim.x);
+      if (w > 8) mbar_wait(bar(Br::kItemEmpty + ((w - 1) & 7)), (uint32_t((w - 1) >> 3) & 1u) ^ 1u, abort_flag, p.status);
+      idx = t < p.n_items_total ? t : -1;
+      ring_idx[(w - 1) & 7] = idx;
+      if (idx >= 0) {
+        const uint4* src = reinterpret_cast<const uint4*>(p.items + idx);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) ring_item[((w - 1) & 7) * 4 + i] = __ldg(src + i);
+      }
+      mbar_arrive(bar(Br::kItemFull + ((w - 1) & 7)));     // (release: the entry is written)
+      if (idx < 0 && atomicAdd(p.queue + 1, 1) == int(gridDim.x) - 1) {   // every CTA has found the queue empty
+        p.queue[0] = 0;
+        p.queue[1] = 0;
+      }
+    }
+    __syncwarp();
+    return __shfl_sync(0xffffffffu, idx, 0) >= 0;
+  };
+  auto next_item = [&](int w) -> bool {                    // the other roles
+    if (w == 0) return true;
+    if (p.queue == nullptr) return false;
+    // a wait that ran out (the CTA is in its error state) ends the CTA's work: no stale entry is used
+    if (!mbar_wait(bar(Br::kItemFull + ((w - 1) & 7)), uint32_t((w - 1) >> 3) & 1u, abort_flag, p.status)) return false;
+    return ring_idx[(w - 1) & 7] >= 0;
+  };
+  const int g = p.group_size;
+  auto halves = [&](const WorkItem& it) { return it.n_nodes * g - it.row0 > BMH ? 2 : 1; };
+
+  trigger_dependents();     // the next kernel of the stream may be scheduled; it waits for this grid before it touches what this one writes
+  if (warp < 4) {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+  if (warp == 0) {
+    // ------------------------------------------------------------------ TMA producer (one lane issues)
+    const bool elected = lane == 0;
+    if (elected) {
+      prefetch_tensormap(&map_q);
+      prefetch_tensormap(&map_k);
+      prefetch_tensormap(&map_v);
+    }
+    uint32_t slot = 0, ph = 0;
+    for (int w = 0; take_item(w); ++w) {
+      const WorkItem item = item_of(w, false);
+      const int nh = halves(item);
+      mbar_wait(bar(Br::kQFree), (uint32_t(w) & 1u) ^ 1u, abort_flag, p.status);
+      // half A, the first K tile, half B: the item's first product needs only the first two
+      auto load_q_half = [&](int h) {
+        if (elected) {
+          mbar_expect_tx(bar(Br::kQFull + h), L::kTileBytes);
+          for (int pn = 0; pn < L::kPanels; ++pn)
+            tma_load_3d(s_q + h * L::kTileBytes + pn * L::kPanelBytes, &map_q, bar(Br::kQFull + h), pn * 64, item.kv_head * g,
+                        item.node0 + ((item.row0 + h * BMH) >> p.log2_g));
+        }
+      };
+      load_q_half(0);
+      for (int t = item.tile_begin; t < item.tile_end; ++t) {
+        const int64_t row = causal_tile_row(p, item, t, BN);
+        for (int kv = 0; kv < 2; ++kv) {
+          mbar_wait(bar(Br::kSlotEmpty + slot), ph ^ 1u, abort_flag, p.status);
+          if (elected) {
+            mbar_expect_tx(bar(Br::kSlotFull + slot), L::kTileBytes);
+            for (int pn = 0; pn < L::kPanels; ++pn)
+              tma_load_3d(s_ring + slot * L::kTileBytes + pn * L::kPanelBytes, kv == 0 ? &map_k : &map_v,
+                          bar(Br::kSlotFull + slot), pn * 64, item.kv_head, int(row));
+          }
+          if (++slot == kSlots) { slot = 0; ph ^= 1u; }
+          if (t == item.tile_begin && kv == 0 && nh == 2) load_q_half(1);
+        }
+      }
+    }
+  } else if (warp == 1 || warp == 3) {
+    // ------------------------------------------------------------------ tcgen05.mma issuers (the elected lane issues)
+    const int h = warp == 1 ? 0 : 1;
+    const bool elected = lane == 0;
+    constexpr uint32_t idesc_qk = make_idesc(BN, 0);
+    constexpr uint32_t idesc_pv = make_idesc(D, 1);
+    constexpr uint32_t kHi = desc_hi(1024);               // 8-row (8-key) groups 1024 bytes apart
+    const uint32_t q_lo0 = desc_lo(s_q, 16) + uint32_t(h) * (L::kTileBytes >> 4);
+    const uint32_t ring_k_lo0 = desc_lo(s_ring, 16);
+    const uint32_t ring_v_lo0 = desc_lo(s_ring, L::kPanelBytes);   // MN-major: leading offset = next 64-column panel
+    const uint32_t t_s = tmem_base + uint32_t(h) * 128u, t_o = tmem_base + 256u + uint32_t(h) * 128u;
+    auto issue_qk = [=](uint32_t slot) {
+      const uint32_t b_lo = ring_k_lo0 + slot * (L::kTileBytes >> 4);
+#pragma unroll
+      for (int ks = 0; ks < D / 16; ++ks) {
+        const uint32_t off = (uint32_t(ks >> 2) * L::kPanelBytes + uint32_t(ks & 3) * 32u) >> 4;
+        if (elected) umma_ss_lohi(t_s, q_lo0 + off, kHi, b_lo + off, kHi, idesc_qk, ks > 0 ? 1u : 0u);
+      }
+    };
+    auto issue_pv = [=](uint32_t slot, int half, bool accumulate) {
+      const uint32_t b_lo = ring_v_lo0 + slot * (L::kTileBytes >> 4);
+#pragma unroll
+      for (int k = 0; k < BN / 32; ++k) {
+        const int kk = half * (BN / 32) + k;
+        if (elected) umma_ts_lohi(t_o, t_s + uint32_t(kk) * 8u, b_lo + uint32_t(kk) * (2048u >> 4), kHi, idesc_pv,
+                                  (accumulate || k > 0) ? 1u : 0u);
+      }
+    };
+    uint32_t slot = 0, ph = 0;                            // ring position
+    uint32_t n_it = 0;                                    // items this half took part in
+    for (int w = 0; next_item(w); ++w) {
+      if (*abort_flag) break;                             // (the softmax warps may have left: nobody to meet at the named barriers)
+      const WorkItem item = item_of(w);
+      const bool two = halves(item) == 2;
+      const int T = item.tile_end - item.tile_begin;
+      if (h == 1 && !two) {                               // no rows for this half: step over the item's tiles
+        slot += 2u * uint32_t(T);
+        ph ^= (slot / kSlots) & 1u;
+        slot %= kSlots;
+        continue;
+      }
+      auto release = [&](int b) {                         // one of the two commits that free a slot / the Q tile
+        if (elected) {
+          tc_commit(bar(b));
+          if (!two) tc_commit(bar(b));
+        }
+      };
+      mbar_wait(bar(Br::kQFull + h), (h == 0 ? uint32_t(w) : n_it) & 1u, abort_flag, p.status);
+      mbar_wait(bar(Br::kSlotFull + slot), ph, abort_flag, p.status);
+      tc_fence_after();
+      issue_qk(slot);
+      if (elected) tc_commit(bar(Br::kSReady + h));
+      release(Br::kSlotEmpty + slot);
+      if (T == 1) release(Br::kQFree);
+      if (++slot == kSlots) { slot = 0; ph ^= 1u; }
+      for (int j = 0; j < T; ++j) {
+        const bool more = j + 1 < T;
+        const uint32_t vslot = slot, vph = ph;
+        if (++slot == kSlots) { slot = 0; ph ^= 1u; }
+        const uint32_t kslot = slot, kph = ph;
+        if (more && ++slot == kSlots) { slot = 0; ph ^= 1u; }
+        const uint32_t got = mbar_test_wait2(bar(Br::kSlotFull + vslot), vph, bar(Br::kSlotFull + (more ? kslot : vslot)), more ? kph : vph);
+        if (!(got & 1u)) mbar_wait(bar(Br::kSlotFull + vslot), vph, abort_flag, p.status);
+        if (more && !(got & 2u)) mbar_wait(bar(Br::kSlotFull + kslot), kph, abort_flag, p.status);
+        if (j == 0) mbar_wait(bar(Br::kOFree + h), (n_it & 1u) ^ 1u, abort_flag, p.status);
+        __syncwarp();
+        named_sync(kBarP + 2 * h, kPCount);
+        tc_fence_after();
+        issue_pv(vslot, 0, j > 0);
+        __syncwarp();
+        named_sync(kBarP + 2 * h + 1, kPCount);
+        tc_fence_after();
+        issue_pv(vslot, 1, true);
+        if (more) {
+          issue_qk(kslot);
+          if (elected) tc_commit(bar(Br::kSReady + h));
+          release(Br::kSlotEmpty + vslot);
+          release(Br::kSlotEmpty + kslot);
+          if (j + 2 == T) release(Br::kQFree);
+        } else {
+          if (elected) tc_commit(bar(Br::kODone + h));
+          release(Br::kSlotEmpty + vslot);
+        }
+      }
+      ++n_it;
+    }
+  }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    // ------------------------------------------------------------------ softmax + epilogue warps
+    // Q, K, V and the work items are inputs that no kernel launched with early start writes; only the output and the
+    // partials wait for the preceding kernels of the stream.
+    bool dep_ok = false;
+    const int h = (warp - 4) >> 2;                       // query half
+    const int r = ((warp & 3) << 5) + lane;              // row of the half == TMEM lane
+    const uint32_t lane_sel = uint32_t((warp & 3) << 5) << 16;
+    const uint32_t t_s = tmem_base + uint32_t(h) * 128u + lane_sel;             // scores, then probabilities (bf16 pairs)
+    const uint32_t t_o = tmem_base + 256u + uint32_t(h) * 128u + lane_sel;
+    uint32_t n_s = 0, n_o = 0;                           // S-ready / O-done phases seen
+    uint32_t slot = 0, ph = 0;                           // ring position of the next K tile (its V tile follows)
+
+    for (int w = 0; next_item(w); ++w) {
+      const WorkItem item = item_of(w);
+      const int n_rows = item.n_nodes * g;
+      const int T = item.tile_end - item.tile_begin;
+      if (h >= halves(item)) {
+        slot += 2u * uint32_t(T);
+        ph ^= (slot / kSlots) & 1u;
+        slot %= kSlots;
+        continue;
+      }
+      const int row = item.row0 + h * BMH + r;
+      const bool ok = row < n_rows;
+      const int token = min(row >> p.log2_g, item.n_nodes - 1);     // (rows behind the last one follow it; they are not written)
+      const int last_key = item.prefix_len + token;                 // the row sees keys 0 .. last_key
+
+      float m_used = -INFINITY, l = 0.f;
+      for (int j = 0; j < T; ++j) {
+        const int key0 = (item.tile_begin + j) * BN;
+        const int vis = last_key + 1 - key0;                        // how many of the tile's keys the row sees (<= 0: none, >= 128: all)
+        const bool all_visible = __all_sync(0xffffffffu, vis >= BN);
+        const int own = item.prefix_len + item.n_nodes - key0;      // how many of them belong to the sequence
+        if (++slot == kSlots) { slot = 0; ph ^= 1u; }               // (slot, ph: now the V tile's)
+        const uint32_t vslot = slot, vph = ph;
+        if (++slot == kSlots) { slot = 0; ph ^= 1u; }
+
+        mbar_wait(bar(Br::kSReady + h), n_s & 1u, abort_flag, p.status);
+        ++n_s;
+        __syncwarp();
+        tc_fence_after();
+        uint32_t sv[BN];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) tmem_ld32(t_s + uint32_t(c) * 32u, sv + 32 * c);
+        tmem_wait_ld();
+        if (!all_visible) {
+#pragma unroll
+          for (int q4 = 0; q4 < 4; ++q4) {
+            const int left = vis - 32 * q4;
+            const uint32_t bits = left >= 32 ? 0xffffffffu : (left <= 0 ? 0u : ((1u << left) - 1u));
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (!((bits >> i) & 1u)) sv[32 * q4 + i] = 0xff800000u;   // -inf
+          }
+        }
+        float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int i = 0; i < BN; i += 8) {
+          mx4[0] = max3_f32(mx4[0], __uint_as_float(sv[i]), __uint_as_float(sv[i + 1]));
+          mx4[1] = max3_f32(mx4[1], __uint_as_float(sv[i + 2]), __uint_as_float(sv[i + 3]));
+          mx4[2] = max3_f32(mx4[2], __uint_as_float(sv[i + 4]), __uint_as_float(sv[i + 5]));
+          mx4[3] = max3_f32(mx4[3], __uint_as_float(sv[i + 6]), __uint_as_float(sv[i + 7]));
+        }
+        const float mx = scaled_maximum(fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])), p.scale_log2e);   // scale > 0
+        const float m_new = fmaxf(m_used, mx);
+        if (j == 0) {
+          m_used = m_new;
+        } else if (__any_sync(0xffffffffu, m_new > m_used + kRescaleThreshold)) {
+          // rescale the running output of this warp's 32 rows: O *= 2^(m_used - m_new)  (P V(j - 1) is done, see above)
+          const float f = fast_exp2(m_used - (m_new == -INFINITY ? 0.f : m_new));
+#pragma unroll 1
+          for (int c = 0; c < D / 32; ++c) {
+            uint32_t v[32];
+            tmem_ld32(t_o + uint32_t(c) * 32u, v);
+            tmem_wait_ld();
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * f);
+            tmem_st32(t_o + uint32_t(c) * 32u, v);
+          }
+          l *= f;
+          m_used = m_new;
+        }
+        const float neg_ref = m_used == -INFINITY ? 0.f : -m_used;
+
+        // V rows behind the end of the sequence are not ours: zero them (their probabilities are 0, but 0 * garbage could be
+        // NaN).  Both halves do, each before it publishes its P: neither's product waits for the other half.
+        if (own < BN) {
+          mbar_wait(bar(Br::kSlotFull + vslot), vph, abort_flag, p.status);
+          uint8_t* v_tile = smem + L::kRingOffset + vslot * L::kTileBytes;
+          for (int idx = r; idx < (BN - own) * 8 * L::kPanels; idx += BMH) {
+            const int pn = idx / ((BN - own) * 8), rem = idx % ((BN - own) * 8);
+            *reinterpret_cast<uint4*>(v_tile + pn * L::kPanelBytes + (own + rem / 8) * 128 + (rem % 8) * 16) = make_uint4(0u, 0u, 0u, 0u);
+          }
+          fence_proxy_async();
+          __syncwarp();
+        }
+
+        // P = 2^(s * scale - ref) as bf16 pairs over the scores (masked: 2^-inf = 0).  The row sum takes P before its rounding.
+        const float scale = scale_for_reference(m_used, p.scale_log2e);
+        const uint64_t scale2 = pack_f32x2(scale, scale), ref2 = pack_f32x2(neg_ref, neg_ref);
+        uint64_t sum2[2] = {0ull, 0ull};
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          uint32_t pk[16];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const uint64_t x = fma_f32x2(pack_f32x2(__uint_as_float(sv[32 * c + 2 * i]), __uint_as_float(sv[32 * c + 2 * i + 1])),
+                                         scale2, ref2);
+            float x0, x1;
+            unpack_f32x2(x, x0, x1);
+            const float p0 = fast_exp2(x0), p1 = fast_exp2(x1);
+            sum2[i & 1] = add_f32x2(sum2[i & 1], pack_f32x2(p0, p1));
+            pk[i] = pack_bf16x2(p0, p1);
+          }
+          tmem_st16(t_s + uint32_t(c) * 16u, pk);
+          if (c & 1) {
+            tmem_wait_st();
+            tc_fence_before();
+            named_arrive(kBarP + 2 * h + (c >> 1), kPCount);
+          }
+        }
+        float a0, a1, b0, b1;
+        unpack_f32x2(sum2[0], a0, a1);
+        unpack_f32x2(sum2[1], b0, b1);
+        l += (a0 + a1) + (b0 + b1);
+      }
+
+      // ---- epilogue: wait for the last P V, read O, normalise (or emit the partial)
+      mbar_wait(bar(Br::kODone + h), n_o & 1u, abort_flag, p.status);
+      ++n_o;
+      __syncwarp();
+      tc_fence_after();
+      if (!dep_ok) {
+        grid_dependency_wait();                            // global writes from here on
+        dep_ok = true;
+      }
+      if (item.slot < 0) {
+        const float inv = l > 0.f ? 1.f / l : 0.f;
+        __nv_bfloat16* out = p.out + (size_t(item.node0 + token) * p.n_q_heads + item.kv_head * g + (row & (g - 1))) * D;
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) {
+          uint32_t v[32];
+          tmem_ld32(t_o + uint32_t(c) * 32u, v);
+          tmem_wait_ld();
+          if (c == D / 32 - 1) { tc_fence_before(); mbar_arrive(bar(Br::kOFree + h)); }
+          if (ok) {
+            uint32_t pk[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) pk[i] = pack_bf16x2(__uint_as_float(v[2 * i]) * inv, __uint_as_float(v[2 * i + 1]) * inv);
+            st_global_v8(out + c * 32, pk);
+            st_global_v8(out + c * 32 + 16, pk + 8);
+          }
+        }
+      } else {
+        // partial slot: O [256][D] fp32, then m [256], then l [256]
+        float* slot_at = p.partial + size_t(item.slot) * p.slot_floats;
+        const int pr = h * BMH + r;
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) {
+          uint32_t v[32];
+          tmem_ld32(t_o + uint32_t(c) * 32u, v);
+          tmem_wait_ld();
+          if (c == D / 32 - 1) { tc_fence_before(); mbar_arrive(bar(Br::kOFree + h)); }
+          if (ok) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) st_global_v8(slot_at + pr * D + c * 32 + 8 * i, v + 8 * i);
+          }
+        }
+        if (ok) {
+          slot_at[2 * BMH * D + pr] = m_used;
+          slot_at[2 * BMH * D + 2 * BMH + pr] = l;
+        }
+      }
+    }
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 2) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(kTmemCols) : "memory");
+  }
+}
+
+namespace {
+template <int D>
+cudaError_t launch_one(cudaLaunchConfig_t& cfg, const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv,
+                       const AttnParams& p, const FirstItems& first) {
+  static DynSmemGrant grant;           // one per instantiation
+  // (padded past half of an SM's shared memory: one CTA per SM, since each CTA takes all 512 TMEM columns)
+  const size_t smem = CausalLayout<D>::kTotal + 1024 > 120 * 1024 ? CausalLayout<D>::kTotal + 1024 : 120 * 1024;
+  if (cudaError_t e = grant.ensure(causal_attn_kernel<D>, smem); e != cudaSuccess) return e;
+  cfg.dynamicSmemBytes = smem;
+  return cudaLaunchKernelEx(&cfg, causal_attn_kernel<D>, mq, mk, mv, p, first);
+}
+}  // namespace
+
+cudaError_t launch_attn_causal(int head_dim, int n_ctas, const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv,
+                               const AttnParams& p, const WorkItem* host_items, cudaStream_t stream) {
+  FirstItems first;                    // host_items: the host copy of p.items; each CTA's first item travels as a kernel parameter
+  for (int c = 0; c < kFirstItems; ++c) first.item[c] = c < n_ctas ? host_items[c] : WorkItem{};
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(unsigned(n_ctas));
+  cfg.blockDim = dim3(unsigned(kThreads));
+  cfg.stream = stream;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  const cudaError_t e = head_dim == 128 ? launch_one<128>(cfg, mq, mk, mv, p, first) : launch_one<64>(cfg, mq, mk, mv, p, first);
+  return e != cudaSuccess ? e : cudaGetLastError();
+}
+
+}  // namespace dyspec

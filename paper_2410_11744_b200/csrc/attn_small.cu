@@ -146,7 +146,9 @@ __device__ __forceinline__ void tmem_st_rows(uint32_t taddr, const float (&v)[NJ
 
 }  // namespace
 
-template <int D>
+// kCausal: causal attention of new tokens (a chunk over its cache, a packed prompt) instead of a tree: node i is token
+// prefix_len + i of the sequence and sees keys 0 .. prefix_len + i; key tiles follow the sequence and no mask is read.
+template <int D, bool kCausal>
 __global__ void __launch_bounds__(kThreads, 1)
 tree_attn_small_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                      const __grid_constant__ CUtensorMap map_v, const AttnParams p,
@@ -260,7 +262,7 @@ tree_attn_small_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
           const uint32_t ph = ring_phase;
           if (++ring_stage == n_stages) { ring_stage = 0; ring_phase ^= 1u; }
           mbar_wait(bar_empty + 8 * stage, ph ^ 1, abort_flag, p.status);
-          const int64_t row = kv_tile_row(p, item, t, n_prefix_tiles, BN);
+          const int64_t row = kCausal ? causal_tile_row(p, item, t, BN) : kv_tile_row(p, item, t, n_prefix_tiles, BN);
           const uint32_t dst = s_kv + stage * L::kStageBytes;
           mbar_expect_tx(bar_full + 8 * stage, L::kStageBytes);
           for (int h = 0; h < L::kHalves; ++h) {
@@ -422,7 +424,7 @@ tree_attn_small_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
       uint2 w_lo = make_uint2(0u, 0u), w_hi = make_uint2(0u, 0u);
       uint2 x_lo = make_uint2(0u, 0u), x_hi = make_uint2(0u, 0u);       // the group in front (shifted tiles only)
       const int shift = tree_tile_shift(rq.prefix_len, BN, p.tree_in_pages);
-      if (t >= n_prefix_tiles) {
+      if (!kCausal && t >= n_prefix_tiles) {
         need_dep();
         const int u = t - n_prefix_tiles;
         const uint2* bits_lo = reinterpret_cast<const uint2*>(p.bits + size_t(rq.node0 + node_lo) * p.words_per_row);
@@ -452,7 +454,14 @@ tree_attn_small_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
       uint64_t vis_lo, vis_hi;
       bool all_visible = false;         // (the same for the whole CTA)
       int own;                          // leading rows of this K/V tile that belong to the request
-      if (t < n_prefix_tiles) {
+      if (kCausal) {
+        const int seen = rq.prefix_len + 1 - t * BN;               // of the tile's keys, by token 0 of the chunk
+        auto leading = [](int n) { return n >= 64 ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1ull; };
+        vis_lo = leading(seen + min(node_lo, rq.n_nodes - 1));
+        vis_hi = leading(seen + min(node_hi, rq.n_nodes - 1));
+        all_visible = seen >= BN;
+        own = min(BN, rq.prefix_len + rq.n_nodes - t * BN);
+      } else if (t < n_prefix_tiles) {
         const int valid = min(BN, rq.prefix_len - t * BN);
         own = min(BN, rq.prefix_len + rq.n_nodes - t * BN);
         const uint64_t m = valid >= 64 ? ~0ull : ((1ull << valid) - 1ull);
@@ -874,11 +883,11 @@ int attn_small_max_clusters(int head_dim, int cluster_size) {
   static DynSmemGrant grant[2];
   cudaError_t e;
   if (head_dim == 128) {
-    e = grant[0].ensure(tree_attn_small_kernel<128>, cfg.dynamicSmemBytes);
-    if (e == cudaSuccess) e = cudaOccupancyMaxActiveClusters(&n, tree_attn_small_kernel<128>, &cfg);
+    e = grant[0].ensure(tree_attn_small_kernel<128, false>, cfg.dynamicSmemBytes);
+    if (e == cudaSuccess) e = cudaOccupancyMaxActiveClusters(&n, tree_attn_small_kernel<128, false>, &cfg);
   } else {
-    e = grant[1].ensure(tree_attn_small_kernel<64>, cfg.dynamicSmemBytes);
-    if (e == cudaSuccess) e = cudaOccupancyMaxActiveClusters(&n, tree_attn_small_kernel<64>, &cfg);
+    e = grant[1].ensure(tree_attn_small_kernel<64, false>, cfg.dynamicSmemBytes);
+    if (e == cudaSuccess) e = cudaOccupancyMaxActiveClusters(&n, tree_attn_small_kernel<64, false>, &cfg);
   }
   if (e != cudaSuccess) { cudaGetLastError(); n = 0; }
   known[dev][hi][ci].store(n + 1);
@@ -893,7 +902,6 @@ cudaError_t launch_attn_small(int head_dim, int n_ctas, const CUtensorMap& mq, c
   for (int c = 0; c < kFirstItems; ++c)
     first.item[c] = c < n_ctas ? host_items[size_t(c) * p.items_stride] : WorkItem{};
   const size_t smem = attn_small_smem_bytes(head_dim);
-  static DynSmemGrant grant[2];
   cudaLaunchAttribute attr[2];
   unsigned n_attr = 0;
   if (early_start) {
@@ -912,16 +920,14 @@ cudaError_t launch_attn_small(int head_dim, int n_ctas, const CUtensorMap& mq, c
   cfg.stream = stream;
   cfg.attrs = attr;
   cfg.numAttrs = n_attr;
-  cudaError_t e = cudaSuccess;
-  if (head_dim == 128) {
-    if (cudaError_t ge = grant[0].ensure(tree_attn_small_kernel<128>, smem); ge != cudaSuccess) return ge;
-    cfg.dynamicSmemBytes = smem;
-    e = cudaLaunchKernelEx(&cfg, tree_attn_small_kernel<128>, mq, mk, mv, p, first);
-  } else {
-    if (cudaError_t ge = grant[1].ensure(tree_attn_small_kernel<64>, smem); ge != cudaSuccess) return ge;
-    cfg.dynamicSmemBytes = smem;
-    e = cudaLaunchKernelEx(&cfg, tree_attn_small_kernel<64>, mq, mk, mv, p, first);
-  }
+  cfg.dynamicSmemBytes = smem;
+  auto launch = [&](auto kernel, DynSmemGrant& grant) {
+    if (cudaError_t ge = grant.ensure(kernel, smem); ge != cudaSuccess) return ge;
+    return cudaLaunchKernelEx(&cfg, kernel, mq, mk, mv, p, first);
+  };
+  static DynSmemGrant grant[4];
+  const cudaError_t e = p.causal ? (head_dim == 128 ? launch(tree_attn_small_kernel<128, true>, grant[2]) : launch(tree_attn_small_kernel<64, true>, grant[3]))
+                                 : (head_dim == 128 ? launch(tree_attn_small_kernel<128, false>, grant[0]) : launch(tree_attn_small_kernel<64, false>, grant[1]));
   return e != cudaSuccess ? e : cudaGetLastError();
 }
 

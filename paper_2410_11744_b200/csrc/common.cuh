@@ -114,6 +114,9 @@ struct AttnParams {
   // queue[1] counts the CTAs that found the queue empty, and the last of them clears both words.
   int32_t* queue;
   int32_t n_items_total;
+  // Causal plans (new tokens of a sequence instead of a tree): n_nodes tokens, token i sees keys 0 .. prefix_len + i.
+  int32_t causal;
+  int64_t kv_total_rows;           // rows of the caches
 };
 
 // Without a grant a launch is held to 48 KB of shared memory, static and dynamic together.  One of these per kernel
@@ -187,6 +190,16 @@ __device__ __forceinline__ int64_t kv_tile_row(const AttnParams& p, const WorkIt
   if (!p.page_table) return it.kv_row0 + s;
   const int32_t page = __ldg(p.page_table + int64_t(it.req) * p.pages_per_req + (s >> p.page_shift));
   return (int64_t(page) << p.page_shift) + (s & ((int64_t(1) << p.page_shift) - 1));
+}
+
+// The same for causal plans, whose key tiles follow the sequence.  A page number outside the pool becomes the row behind the
+// last one, where a TMA load reads zeros.
+__device__ __forceinline__ int64_t causal_tile_row(const AttnParams& p, const WorkItem& it, int t, int BN) {
+  const int64_t s = int64_t(t) * BN;
+  if (!p.page_table) return it.kv_row0 + s;
+  const int64_t page = __ldg(p.page_table + int64_t(it.req) * p.pages_per_req + (s >> p.page_shift));
+  const int64_t row0 = page << p.page_shift;
+  return page < 0 || row0 >= p.kv_total_rows ? p.kv_total_rows : row0 + (s & ((int64_t(1) << p.page_shift) - 1));
 }
 
 // ------------------------------------------------------------------------------------------------
