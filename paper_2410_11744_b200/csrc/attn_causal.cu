@@ -5,18 +5,22 @@
 // One CTA per SM, 12 warps; a work item is 256 packed query rows of one (request, kv head), two halves A and B of 128, against
 // a range of 128-key tiles:
 //   warp 0       TMA producer: the item's Q (half A, then B), then K and V tiles into a shared-memory ring;
-//   warps 1, 3   tcgen05.mma issuers of half A / B: S = Q K^T (both operands in shared memory), O += P V (P in tensor memory);
+//   warp 1       issues tcgen05.mma: S = Q K^T (both operands in shared memory), O += P V (P in tensor memory);
 //   warp 2       tensor memory: S_A, S_B (128 fp32 columns each), O_A, O_B (D each);
 //   warps 4-7    softmax of half A, a row per thread: fp32 online softmax in the exp2 domain; warps 8-11 of half B.
 // A half's P (bf16) takes the place of its S: a thread has its row of scores in registers before it writes the first
 // probability.  Products of one issuing thread run in order, so S(j + 1), issued behind P V(j), overwrites a P that has
 // been read, and "S(j + 1) is there" also says that P V(j) is done: one barrier tells the softmax threads both, and the
-// running output may be rescaled then without another wait.  The tensor pipe works for the other half meanwhile.
+// running output may be rescaled then without another wait.  One thread issues for both halves: P V and the next S of A, then
+// those of B, and so on, and the softmax of one half runs under the products of the other.  (An issuer per half, as in the tree
+// kernel, has its products interleaved with the other's: both halves' S arrive together, both softmaxes run at once and the
+// pipe waits for them, 4 430 cycles a tile.)
 // P is handed over in two pieces of 64 keys, so that the first half of P V runs under the second half of the exponentials.
 //
 // CTAs take items from a queue, longest first (see schedule_causal in api.cu); an item whose group was cut along the
 // keys writes an fp32 partial (O, m, l) that combine_kernel merges.  Every wait on an mbarrier is bounded (see mbar_wait).
 #include "tc_ops.cuh"
+#include <type_traits>
 
 namespace dyspec {
 
@@ -44,9 +48,9 @@ struct CausalLayout {
 template <int kSlots>
 struct Bars {
   static constexpr int kQFull = 0;                      // [2] query half A / B is in shared memory
-  static constexpr int kQFree = 2;                      // both halves' last S products have run
+  static constexpr int kQFree = 2;                      // the item's last S products have run
   static constexpr int kSlotFull = 3;                   // [kSlots]
-  static constexpr int kSlotEmpty = kSlotFull + kSlots; // [kSlots] two commits, one per half
+  static constexpr int kSlotEmpty = kSlotFull + kSlots; // [kSlots]
   static constexpr int kSReady = kSlotEmpty + kSlots;   // [2]
   static constexpr int kODone = kSReady + 2;            // [2] the item's last P V has run
   static constexpr int kOFree = kODone + 2;             // [2] the output has been read out
@@ -55,6 +59,61 @@ struct Bars {
   static constexpr int kCount = kItemEmpty + 8;
 };
 
+// 2^x for x <= 127 on the FMA pipe, two at a time: x = n + f with n the nearest integer, 2^f by the cubic with the smallest
+// largest relative error on [-1/2, 1/2] (7.5e-5, found by Remez exchange; P is rounded to bf16, 2^-9, right behind it), n
+// added to its exponent.  Below -125 the result stays at 2^-125 (relative to a row's largest term of 1, nothing); a NaN is
+// the caller's to keep away.
+__device__ __forceinline__ uint64_t exp2_poly2(uint64_t x2) {
+  constexpr float kMagic = 12582912.f;      // 1.5 * 2^23: adding it leaves the nearest integer in the low bits
+  float x0, x1, t0, t1, p0, p1;
+  unpack_f32x2(x2, x0, x1);
+  x2 = pack_f32x2(fmaxf(x0, -125.f), fmaxf(x1, -125.f));
+  const uint64_t t2 = add_f32x2(x2, pack_f32x2(kMagic, kMagic));
+  const uint64_t n2 = add_f32x2(t2, pack_f32x2(-kMagic, -kMagic));
+  const uint64_t f2 = fma_f32x2(n2, pack_f32x2(-1.f, -1.f), x2);
+  uint64_t p2 = fma_f32x2(pack_f32x2(0.0551716685f, 0.0551716685f), f2, pack_f32x2(0.242611125f, 0.242611125f));
+  p2 = fma_f32x2(p2, f2, pack_f32x2(0.693260968f, 0.693260968f));
+  p2 = fma_f32x2(p2, f2, pack_f32x2(0.999928057f, 0.999928057f));
+  unpack_f32x2(t2, t0, t1);
+  unpack_f32x2(p2, p0, p1);
+  return pack_f32x2(__uint_as_float(__float_as_uint(p0) + (__float_as_uint(t0) << 23)),
+                    __uint_as_float(__float_as_uint(p1) + (__float_as_uint(t1) << 23)));
+}
+#ifndef REG_LO
+#define REG_LO "64"
+#define REG_HI "216"
+#endif
+#ifndef POLY
+#define POLY 4
+#endif
+constexpr int kPolyPairs = POLY;             // of the 16 pairs in 32 keys, how many take the polynomial
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+  return d;
+}
+
+// Trace tags (see dyspec_set_trace): role << 14 | event << 10 | key-tile index; role 0 = issuer, 1 / 2 = softmax row 0 of half A / B.
+// Issuer events (half B: + 4): 1 / 3 first / second 64 keys of P seen, 2 P V issued, 4 next S issued.  Softmax events: 1 S seen, 2
+// row loaded, 3 maximum known, 4 / 5 first / second 64 keys of P published.
+#define DYSPEC_TAG(role, event, j) ((uint32_t(role) << 14) | (uint32_t(event) << 10) | (uint32_t(j) & 1023u))
+
+// One lane of the warp, and the compiler knows that it is one: what feeds a tcgen05 instruction stays in uniform registers.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t one;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one) :: "memory");
+  return one != 0;
+}
+
+#ifndef SPLIT
+#define SPLIT 2
+#endif
+constexpr int kFirstChunks = SPLIT;          // P is handed over in two pieces: 32 * kFirstChunks keys, then the rest
 constexpr int kBarP = 1;                    // named barriers 1 .. 4: 64 keys of P are in tensor memory (half A: 1, 2; half B: 3, 4)
 constexpr int kPCount = BMH + 32;           // a half's softmax threads + the issuing warp
 
@@ -79,7 +138,7 @@ causal_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
   volatile int32_t* ring_idx = reinterpret_cast<volatile int32_t*>(smem + L::kBarOffset + 8 * Br::kCount + 16);
   uint4* ring_item = reinterpret_cast<uint4*>(smem + L::kItemRingOffset);
 
-  const int warp = threadIdx.x >> 5;
+  const int warp = __shfl_sync(0xffffffffu, int(threadIdx.x >> 5), 0);
   const int lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int h = 0; h < 2; ++h) {
@@ -88,14 +147,14 @@ causal_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
       mbar_init(bar(Br::kODone + h), 1);
       mbar_init(bar(Br::kOFree + h), BMH);
     }
-    mbar_init(bar(Br::kQFree), 2);
+    mbar_init(bar(Br::kQFree), 1);
     for (int s = 0; s < kSlots; ++s) {
       mbar_init(bar(Br::kSlotFull + s), 1);
-      mbar_init(bar(Br::kSlotEmpty + s), 2);
+      mbar_init(bar(Br::kSlotEmpty + s), 1);
     }
     for (int e = 0; e < 8; ++e) {
       mbar_init(bar(Br::kItemFull + e), 1);
-      mbar_init(bar(Br::kItemEmpty + e), 2 + 2 * BMH / 32);
+      mbar_init(bar(Br::kItemEmpty + e), 1 + 2 * BMH / 32);
     }
     *abort_flag = 0;
     fence_barrier_init();
@@ -108,7 +167,7 @@ causal_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem_base = *tmem_holder;
+  const uint32_t tmem_base = __shfl_sync(0xffffffffu, *tmem_holder, 0);
 
   // The CTA's first item is item blockIdx.x of the queue and travels with the kernel parameters; the producer warp takes
   // further ones with an atomic add and passes them on through a ring of 8 entries.  No queue (p.queue null): one item per CTA.
@@ -151,8 +210,14 @@ causal_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
   auto next_item = [&](int w) -> bool {                    // the other roles
     if (w == 0) return true;
     if (p.queue == nullptr) return false;
-    // a wait that ran out (the CTA is in its error state) ends the CTA's work: no stale entry is used
-    if (!mbar_wait(bar(Br::kItemFull + ((w - 1) & 7)), uint32_t((w - 1) >> 3) & 1u, abort_flag, p.status)) return false;
+    // The producer publishes every item in bounded time, whatever other waits ran out: a role that is in its error state still
+    // goes through the items that the others go through, so that all of them meet at the named barriers.
+    const uint32_t at = bar(Br::kItemFull + ((w - 1) & 7)), parity = uint32_t((w - 1) >> 3) & 1u;
+    if (!mbar_wait(at, parity, abort_flag, p.status)) {
+      const uint64_t t0 = global_timer_ns();
+      while (!mbar_test_wait(at, parity))
+        if (global_timer_ns() - t0 > 8 * kWaitLimitNs) return false;
+    }
     return ring_idx[(w - 1) & 7] >= 0;
   };
   const int g = p.group_size;
@@ -160,7 +225,7 @@ causal_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 
   trigger_dependents();     // the next kernel of the stream may be scheduled; it waits for this grid before it touches what this one writes
   if (warp < 4) {
-  asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 " REG_LO ";");
   if (warp == 0) {
     // ------------------------------------------------------------------ TMA producer (one lane issues)
     const bool elected = lane == 0;
@@ -199,95 +264,104 @@ causal_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         }
       }
     }
-  } else if (warp == 1 || warp == 3) {
-    // ------------------------------------------------------------------ tcgen05.mma issuers (the elected lane issues)
-    const int h = warp == 1 ? 0 : 1;
+  } else if (warp == 1) {
+    // ------------------------------------------------------------------ tcgen05.mma issuer (one lane issues)
     const bool elected = lane == 0;
+    TraceCursor trace = trace_open(p, 0, 3);
+    if (!elected) trace.at = nullptr;
     constexpr uint32_t idesc_qk = make_idesc(BN, 0);
     constexpr uint32_t idesc_pv = make_idesc(D, 1);
     constexpr uint32_t kHi = desc_hi(1024);               // 8-row (8-key) groups 1024 bytes apart
-    const uint32_t q_lo0 = desc_lo(s_q, 16) + uint32_t(h) * (L::kTileBytes >> 4);
+    const uint32_t q_lo0 = desc_lo(s_q, 16);
     const uint32_t ring_k_lo0 = desc_lo(s_ring, 16);
     const uint32_t ring_v_lo0 = desc_lo(s_ring, L::kPanelBytes);   // MN-major: leading offset = next 64-column panel
-    const uint32_t t_s = tmem_base + uint32_t(h) * 128u, t_o = tmem_base + 256u + uint32_t(h) * 128u;
-    auto issue_qk = [=](uint32_t slot) {
-      const uint32_t b_lo = ring_k_lo0 + slot * (L::kTileBytes >> 4);
+    auto issue_qk = [=](int h, uint32_t slot) {
+      const uint32_t a_lo = q_lo0 + uint32_t(h) * (L::kTileBytes >> 4);
+      const uint32_t b_lo = ring_k_lo0 + __shfl_sync(0xffffffffu, slot, 0) * (L::kTileBytes >> 4);
+      if (elect_one()) {
 #pragma unroll
-      for (int ks = 0; ks < D / 16; ++ks) {
-        const uint32_t off = (uint32_t(ks >> 2) * L::kPanelBytes + uint32_t(ks & 3) * 32u) >> 4;
-        if (elected) umma_ss_lohi(t_s, q_lo0 + off, kHi, b_lo + off, kHi, idesc_qk, ks > 0 ? 1u : 0u);
-      }
-    };
-    auto issue_pv = [=](uint32_t slot, int half, bool accumulate) {
-      const uint32_t b_lo = ring_v_lo0 + slot * (L::kTileBytes >> 4);
-#pragma unroll
-      for (int k = 0; k < BN / 32; ++k) {
-        const int kk = half * (BN / 32) + k;
-        if (elected) umma_ts_lohi(t_o, t_s + uint32_t(kk) * 8u, b_lo + uint32_t(kk) * (2048u >> 4), kHi, idesc_pv,
-                                  (accumulate || k > 0) ? 1u : 0u);
-      }
-    };
-    uint32_t slot = 0, ph = 0;                            // ring position
-    uint32_t n_it = 0;                                    // items this half took part in
-    for (int w = 0; next_item(w); ++w) {
-      if (*abort_flag) break;                             // (the softmax warps may have left: nobody to meet at the named barriers)
-      const WorkItem item = item_of(w);
-      const bool two = halves(item) == 2;
-      const int T = item.tile_end - item.tile_begin;
-      if (h == 1 && !two) {                               // no rows for this half: step over the item's tiles
-        slot += 2u * uint32_t(T);
-        ph ^= (slot / kSlots) & 1u;
-        slot %= kSlots;
-        continue;
-      }
-      auto release = [&](int b) {                         // one of the two commits that free a slot / the Q tile
-        if (elected) {
-          tc_commit(bar(b));
-          if (!two) tc_commit(bar(b));
+        for (int ks = 0; ks < D / 16; ++ks) {
+          const uint32_t off = (uint32_t(ks >> 2) * L::kPanelBytes + uint32_t(ks & 3) * 32u) >> 4;
+          umma_ss_lohi(tmem_base + uint32_t(h) * 128u, a_lo + off, kHi, b_lo + off, kHi, idesc_qk, ks > 0 ? 1u : 0u);
         }
-      };
-      mbar_wait(bar(Br::kQFull + h), (h == 0 ? uint32_t(w) : n_it) & 1u, abort_flag, p.status);
+      }
+      __syncwarp();
+    };
+    auto issue_pv = [=](int h, uint32_t slot, auto piece_tag, bool accumulate) {
+      constexpr int kFrom = decltype(piece_tag)::value ? 2 * kFirstChunks : 0, kTo = decltype(piece_tag)::value ? BN / 16 : 2 * kFirstChunks;
+      const uint32_t b_lo = ring_v_lo0 + __shfl_sync(0xffffffffu, slot, 0) * (L::kTileBytes >> 4);
+      if (elect_one()) {
+#pragma unroll
+        for (int kk = kFrom; kk < kTo; ++kk) {
+          umma_ts_lohi(tmem_base + 256u + uint32_t(h) * 128u, tmem_base + uint32_t(h) * 128u + uint32_t(kk) * 8u,
+                       b_lo + uint32_t(kk) * (2048u >> 4), kHi, idesc_pv, (accumulate || kk > kFrom) ? 1u : 0u);
+        }
+      }
+      __syncwarp();
+    };
+    auto commit = [&](int b) { if (elect_one()) tc_commit(bar(b)); };
+    constexpr uint32_t kNone = 0xffffffffu;
+    uint32_t slot = 0, ph = 0;                            // ring position
+    uint32_t n_two = 0;                                   // items with both halves
+    for (int w = 0; next_item(w); ++w) {
+      const WorkItem item = item_of(w);
+      const int nh = halves(item);
+      const int T = item.tile_end - item.tile_begin;
       mbar_wait(bar(Br::kSlotFull + slot), ph, abort_flag, p.status);
-      tc_fence_after();
-      issue_qk(slot);
-      if (elected) tc_commit(bar(Br::kSReady + h));
-      release(Br::kSlotEmpty + slot);
-      if (T == 1) release(Br::kQFree);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        if (h >= nh) break;
+        mbar_wait(bar(Br::kQFull + h), (h == 0 ? uint32_t(w) : n_two) & 1u, abort_flag, p.status);
+        __syncwarp();
+        tc_fence_after();
+        issue_qk(h, slot);
+        commit(Br::kSReady + h);
+      }
+      commit(Br::kSlotEmpty + slot);
+      if (T == 1) commit(Br::kQFree);
       if (++slot == kSlots) { slot = 0; ph ^= 1u; }
+      // What runs between two batches of products is time that the pipe stands still: barriers are looked at where the issuer
+      // would wait for the second half of P anyway, the next K tile's in half A's turn, the next V tile's in the last one's.
+      bool v_here = false;
+      uint32_t freed = kNone;                             // the K slot that the last S products read, released behind the next batch
       for (int j = 0; j < T; ++j) {
         const bool more = j + 1 < T;
         const uint32_t vslot = slot, vph = ph;
         if (++slot == kSlots) { slot = 0; ph ^= 1u; }
         const uint32_t kslot = slot, kph = ph;
         if (more && ++slot == kSlots) { slot = 0; ph ^= 1u; }
-        const uint32_t got = mbar_test_wait2(bar(Br::kSlotFull + vslot), vph, bar(Br::kSlotFull + (more ? kslot : vslot)), more ? kph : vph);
-        if (!(got & 1u)) mbar_wait(bar(Br::kSlotFull + vslot), vph, abort_flag, p.status);
-        if (more && !(got & 2u)) mbar_wait(bar(Br::kSlotFull + kslot), kph, abort_flag, p.status);
-        if (j == 0) mbar_wait(bar(Br::kOFree + h), (n_it & 1u) ^ 1u, abort_flag, p.status);
-        __syncwarp();
-        named_sync(kBarP + 2 * h, kPCount);
-        tc_fence_after();
-        issue_pv(vslot, 0, j > 0);
-        __syncwarp();
-        named_sync(kBarP + 2 * h + 1, kPCount);
-        tc_fence_after();
-        issue_pv(vslot, 1, true);
-        if (more) {
-          issue_qk(kslot);
-          if (elected) tc_commit(bar(Br::kSReady + h));
-          release(Br::kSlotEmpty + vslot);
-          release(Br::kSlotEmpty + kslot);
-          if (j + 2 == T) release(Br::kQFree);
-        } else {
-          if (elected) tc_commit(bar(Br::kODone + h));
-          release(Br::kSlotEmpty + vslot);
+        if (!v_here) mbar_wait(bar(Br::kSlotFull + vslot), vph, abort_flag, p.status);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          if (h >= nh) break;
+          if (j == 0) mbar_wait(bar(Br::kOFree + h), ((h == 0 ? uint32_t(w) : n_two) & 1u) ^ 1u, abort_flag, p.status);
+          __syncwarp();
+          named_sync(kBarP + 2 * h, kPCount);
+          tc_fence_after();
+          trace_event(trace, DYSPEC_TAG(0, 1 + 4 * h, j));
+          issue_pv(h, vslot, std::integral_constant<int, 0>{}, j > 0);
+          if (h == 0 && freed != kNone) commit(Br::kSlotEmpty + freed);
+          if (h == 0 && more) mbar_wait(bar(Br::kSlotFull + kslot), kph, abort_flag, p.status);
+          if (h + 1 == nh && more) v_here = mbar_test_wait(bar(Br::kSlotFull + slot), ph);
+          __syncwarp();
+          named_sync(kBarP + 2 * h + 1, kPCount);
+          tc_fence_after();
+          trace_event(trace, DYSPEC_TAG(0, 3 + 4 * h, j));
+          issue_pv(h, vslot, std::integral_constant<int, 1>{}, true);
+          trace_event(trace, DYSPEC_TAG(0, 2 + 4 * h, j));
+          if (h + 1 == nh) commit(Br::kSlotEmpty + vslot);
+          if (more) issue_qk(h, kslot);
+          commit(more ? Br::kSReady + h : Br::kODone + h);
+          trace_event(trace, DYSPEC_TAG(0, 4 + 4 * h, j));
         }
+        freed = more ? kslot : kNone;
+        if (j + 2 == T) { commit(Br::kQFree); commit(Br::kSlotEmpty + kslot); freed = kNone; }
       }
-      ++n_it;
+      n_two += nh == 2 ? 1u : 0u;
     }
   }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 " REG_HI ";");
     // ------------------------------------------------------------------ softmax + epilogue warps
     // Q, K, V and the work items are inputs that no kernel launched with early start writes; only the output and the
     // partials wait for the preceding kernels of the stream.
@@ -299,6 +373,8 @@ causal_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     const uint32_t t_o = tmem_base + 256u + uint32_t(h) * 128u + lane_sel;
     uint32_t n_s = 0, n_o = 0;                           // S-ready / O-done phases seen
     uint32_t slot = 0, ph = 0;                           // ring position of the next K tile (its V tile follows)
+    TraceCursor trace = trace_open(p, 1 + h, 3);
+    if (r != 0) trace.at = nullptr;
 
     for (int w = 0; next_item(w); ++w) {
       const WorkItem item = item_of(w);
@@ -329,10 +405,12 @@ causal_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         ++n_s;
         __syncwarp();
         tc_fence_after();
+        trace_event(trace, DYSPEC_TAG(1 + h, 1, j));
         uint32_t sv[BN];
 #pragma unroll
         for (int c = 0; c < 4; ++c) tmem_ld32(t_s + uint32_t(c) * 32u, sv + 32 * c);
         tmem_wait_ld();
+        trace_event(trace, DYSPEC_TAG(1 + h, 2, j));
         if (!all_visible) {
 #pragma unroll
           for (int q4 = 0; q4 < 4; ++q4) {
@@ -346,69 +424,106 @@ causal_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         float mx4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
         for (int i = 0; i < BN; i += 8) {
-          mx4[0] = max3_f32(mx4[0], __uint_as_float(sv[i]), __uint_as_float(sv[i + 1]));
-          mx4[1] = max3_f32(mx4[1], __uint_as_float(sv[i + 2]), __uint_as_float(sv[i + 3]));
-          mx4[2] = max3_f32(mx4[2], __uint_as_float(sv[i + 4]), __uint_as_float(sv[i + 5]));
-          mx4[3] = max3_f32(mx4[3], __uint_as_float(sv[i + 6]), __uint_as_float(sv[i + 7]));
+          mx4[0] = max3_nan(mx4[0], __uint_as_float(sv[i]), __uint_as_float(sv[i + 1]));
+          mx4[1] = max3_nan(mx4[1], __uint_as_float(sv[i + 2]), __uint_as_float(sv[i + 3]));
+          mx4[2] = max3_nan(mx4[2], __uint_as_float(sv[i + 4]), __uint_as_float(sv[i + 5]));
+          mx4[3] = max3_nan(mx4[3], __uint_as_float(sv[i + 6]), __uint_as_float(sv[i + 7]));
         }
-        const float mx = scaled_maximum(fmaxf(fmaxf(mx4[0], mx4[1]), fmaxf(mx4[2], mx4[3])), p.scale_log2e);   // scale > 0
-        const float m_new = fmaxf(m_used, mx);
-        if (j == 0) {
-          m_used = m_new;
-        } else if (__any_sync(0xffffffffu, m_new > m_used + kRescaleThreshold)) {
-          // rescale the running output of this warp's 32 rows: O *= 2^(m_used - m_new)  (P V(j - 1) is done, see above)
-          const float f = fast_exp2(m_used - (m_new == -INFINITY ? 0.f : m_new));
-#pragma unroll 1
-          for (int c = 0; c < D / 32; ++c) {
-            uint32_t v[32];
-            tmem_ld32(t_o + uint32_t(c) * 32u, v);
-            tmem_wait_ld();
-#pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * f);
-            tmem_st32(t_o + uint32_t(c) * 32u, v);
-          }
-          l *= f;
-          m_used = m_new;
-        }
-        const float neg_ref = m_used == -INFINITY ? 0.f : -m_used;
+        const float mx = scaled_maximum(max3_nan(max_nan(mx4[0], mx4[1]), mx4[2], mx4[3]), p.scale_log2e);   // scale > 0
+        const float m_new = max_nan(m_used, mx);
 
-        // V rows behind the end of the sequence are not ours: zero them (their probabilities are 0, but 0 * garbage could be
-        // NaN).  Both halves do, each before it publishes its P: neither's product waits for the other half.
-        if (own < BN) {
-          mbar_wait(bar(Br::kSlotFull + vslot), vph, abort_flag, p.status);
-          uint8_t* v_tile = smem + L::kRingOffset + vslot * L::kTileBytes;
-          for (int idx = r; idx < (BN - own) * 8 * L::kPanels; idx += BMH) {
-            const int pn = idx / ((BN - own) * 8), rem = idx % ((BN - own) * 8);
-            *reinterpret_cast<uint4*>(v_tile + pn * L::kPanelBytes + (own + rem / 8) * 128 + (rem % 8) * 16) = make_uint4(0u, 0u, 0u, 0u);
-          }
-          fence_proxy_async();
-          __syncwarp();
-        }
-
-        // P = 2^(s * scale - ref) as bf16 pairs over the scores (masked: 2^-inf = 0).  The row sum takes P before its rounding.
-        const float scale = scale_for_reference(m_used, p.scale_log2e);
-        const uint64_t scale2 = pack_f32x2(scale, scale), ref2 = pack_f32x2(neg_ref, neg_ref);
+        // P = 2^(s * scale - ref) as bf16 pairs over the scores (masked: 2^-inf = 0), 64 keys at a time.  The row sum takes P before its
+        // rounding.  The exponential unit takes 8 cycles per warp and instruction, as long for a tile as the tensor pipe, so a
+        // share of the keys takes the polynomial -- where all keys are visible and no row's reference is infinite, NaN or coarse.
         uint64_t sum2[2] = {0ull, 0ull};
+        auto weights = [&](auto half_tag, auto poly_tag, float scale, float neg_ref) {
+          constexpr int kHalf = decltype(half_tag)::value, kPoly = decltype(poly_tag)::value;
+          const uint64_t scale2 = pack_f32x2(scale, scale), ref2 = pack_f32x2(neg_ref, neg_ref);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          uint32_t pk[16];
+          for (int c = kHalf ? kFirstChunks : 0; c < (kHalf ? 4 : kFirstChunks); ++c) {
+            uint32_t pk[16];
+            uint64_t xs[16];
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const uint64_t x = fma_f32x2(pack_f32x2(__uint_as_float(sv[32 * c + 2 * i]), __uint_as_float(sv[32 * c + 2 * i + 1])),
-                                         scale2, ref2);
-            float x0, x1;
-            unpack_f32x2(x, x0, x1);
-            const float p0 = fast_exp2(x0), p1 = fast_exp2(x1);
-            sum2[i & 1] = add_f32x2(sum2[i & 1], pack_f32x2(p0, p1));
-            pk[i] = pack_bf16x2(p0, p1);
+            for (int i = 0; i < 16; ++i)
+              xs[i] = fma_f32x2(pack_f32x2(__uint_as_float(sv[32 * c + 2 * i]), __uint_as_float(sv[32 * c + 2 * i + 1])), scale2, ref2);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              if ((i + 1) * kPoly / 16 > i * kPoly / 16) {
+                xs[i] = exp2_poly2(xs[i]);
+              } else {
+                float p0, p1;
+                unpack_f32x2(xs[i], p0, p1);
+                xs[i] = pack_f32x2(fast_exp2(p0), fast_exp2(p1));
+              }
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              float p0, p1;
+              sum2[i & 1] = add_f32x2(sum2[i & 1], xs[i]);
+              unpack_f32x2(xs[i], p0, p1);
+              pk[i] = pack_bf16x2(p0, p1);
+            }
+            tmem_st16(t_s + uint32_t(c) * 16u, pk);
           }
-          tmem_st16(t_s + uint32_t(c) * 16u, pk);
-          if (c & 1) {
-            tmem_wait_st();
-            tc_fence_before();
-            named_arrive(kBarP + 2 * h + (c >> 1), kPCount);
-          }
+        };
+        auto publish = [&](int half) {
+          tmem_wait_st();
+          tc_fence_before();
+          named_arrive(kBarP + 2 * h + half, kPCount);
+          trace_event(trace, DYSPEC_TAG(1 + h, 4 + half, j));
+        };
+        constexpr std::integral_constant<int, 0> kFirst{}, kExact{};
+        constexpr std::integral_constant<int, 1> kSecond{};
+        constexpr std::integral_constant<int, kPolyPairs> kMixed{};
+        // The reference almost always stays: the first weights are computed against the one there is, beside the maximum
+        // instead of behind it, and again in the rare tile that raises it.
+        bool careful = j == 0 || !all_visible || !__all_sync(0xffffffffu, fabsf(m_used) <= kCoarseReference);
+        if (!careful) {
+          weights(kFirst, kMixed, p.scale_log2e, -m_used);
+          careful = __any_sync(0xffffffffu, !(m_new <= m_used + kRescaleThreshold));
         }
+        trace_event(trace, DYSPEC_TAG(1 + h, 3, j));
+        if (!careful) {
+          publish(0);
+          weights(kSecond, kMixed, p.scale_log2e, -m_used);
+        } else {
+          if (j == 0) {
+            m_used = m_new;
+          } else if (__any_sync(0xffffffffu, !(m_new <= m_used + kRescaleThreshold))) {
+            // rescale the running output of this warp's 32 rows: O *= 2^(m_used - m_new)  (P V(j - 1) is done, see above)
+            const float f = fast_exp2(m_used - (m_new == -INFINITY ? 0.f : m_new));
+#pragma unroll 1
+            for (int c = 0; c < D / 32; ++c) {
+              uint32_t v[32];
+              tmem_ld32(t_o + uint32_t(c) * 32u, v);
+              tmem_wait_ld();
+#pragma unroll
+              for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * f);
+              tmem_st32(t_o + uint32_t(c) * 32u, v);
+            }
+            l *= f;
+            m_used = m_new;
+          }
+          // V rows behind the end of the sequence are not ours: zero them (their probabilities are 0, but 0 * garbage could be
+          // NaN).  Both halves do, each before it publishes its P: neither's product waits for the other half.
+          if (own < BN) {
+            mbar_wait(bar(Br::kSlotFull + vslot), vph, abort_flag, p.status);
+            uint8_t* v_tile = smem + L::kRingOffset + vslot * L::kTileBytes;
+            for (int idx = r; idx < (BN - own) * 8 * L::kPanels; idx += BMH) {
+              const int pn = idx / ((BN - own) * 8), rem = idx % ((BN - own) * 8);
+              *reinterpret_cast<uint4*>(v_tile + pn * L::kPanelBytes + (own + rem / 8) * 128 + (rem % 8) * 16) = make_uint4(0u, 0u, 0u, 0u);
+            }
+            fence_proxy_async();
+            __syncwarp();
+          }
+          sum2[0] = sum2[1] = 0ull;
+          const float scale = scale_for_reference(m_used, p.scale_log2e);
+          const float neg_ref = m_used == -INFINITY ? 0.f : -m_used;
+          weights(kFirst, kExact, scale, neg_ref);
+          publish(0);
+          weights(kSecond, kExact, scale, neg_ref);
+        }
+        publish(1);
         float a0, a1, b0, b1;
         unpack_f32x2(sum2[0], a0, a1);
         unpack_f32x2(sum2[1], b0, b1);
