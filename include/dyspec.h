@@ -499,14 +499,20 @@ int dyspec_compact_kv_paged(void* k_cache, void* v_cache, const int64_t* tree_ro
  *   status           dev int32 [1] or NULL: DYSPEC_ERR_INVALID_ARG when a token has no page, a row outside the pool or a
  *                    position outside the table; nothing of such a token is written, the others are.
  * Two new tokens with the same pool row are the caller's mistake (either may win).
+ * args: host, only read during the call.
  */
-int dyspec_append_kv_paged(const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride, const void* q,
-                           int64_t q_stride, void* q_out, int64_t q_out_stride, int n_q_heads, void* k_cache, void* v_cache,
-                           int64_t kv_total_rows, const int32_t* token_offsets, const int32_t* context_len,
-                           const int32_t* depths, const int64_t* tree_row_offset, int n_req, int n_tokens,
-                           const int32_t* page_table, int pages_per_req, int page_size, const float* rope_table,
-                           int n_positions, int rotary_dim, int interleaved, int n_kv_heads, int head_dim, int32_t* status,
-                           dyspec_stream_t stream);
+typedef struct dyspec_append {
+  const void *k_new, *v_new, *q;
+  void *q_out, *k_cache, *v_cache;
+  int64_t k_stride, v_stride, q_stride, q_out_stride, kv_total_rows;
+  const int32_t *token_offsets, *context_len, *depths;
+  const int64_t* tree_row_offset;
+  const int32_t* page_table;
+  const float* rope_table;
+  int32_t* status;
+  int32_t n_req, n_tokens, n_q_heads, n_kv_heads, head_dim, pages_per_req, page_size, n_positions, rotary_dim, interleaved;
+} dyspec_append_t;
+int dyspec_append_kv_paged(const dyspec_append_t* args, dyspec_stream_t stream);
 
 /*
  * (10) Causal attention of new tokens: what a step computes for requests that bring no tree (a prompt, a chunk of one, the single

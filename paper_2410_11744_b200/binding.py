@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional, Sequence
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -57,8 +58,7 @@ SIGNATURES = {
     "dyspec_plan_create_paged": (_i32, [_c.POINTER(_vp), _i32, _i32, _i32, _i32, _vp, _vp, _vp, _i64, _i32, _i32, _f32]),
     "dyspec_tree_attention_paged": (_i32, [_vp, _vp, _vp, _vp, _vp, _i32, _vp, _vp, _vp, _vp, _sz, _vp, _vp]),
     "dyspec_compact_kv_paged": (_i32, [_vp, _vp, _vp, _vp, _i32, _i32, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _i32, _vp, _vp, _vp]),
-    "dyspec_append_kv_paged": (_i32, [_vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _i32, _vp, _vp, _i64, _vp, _vp, _vp, _vp, _i32, _i32,
-                                      _vp, _i32, _i32, _vp, _i32, _i32, _i32, _i32, _i32, _vp, _vp]),
+    "dyspec_append_kv_paged": (_i32, [_c.c_char_p, _vp]),
     "dyspec_plan_create_chunk": (_i32, [_c.POINTER(_vp), _i32, _i32, _i32, _i32, _vp, _vp, _i64, _i32, _f32]),
     "dyspec_chunk_attention_paged": (_i32, [_vp, _vp, _i64, _vp, _vp, _vp, _i32, _vp, _vp, _sz, _vp, _vp]),
     "dyspec_plan_create_prompt": (_i32, [_c.POINTER(_vp), _i32, _i32, _i32, _i32, _vp, _f32]),
@@ -429,6 +429,10 @@ def dyspec_prompt_attention(plan: Plan, q, k, v, out, workspace=None, status=Non
                                        _ptr(workspace), ws_bytes, _ptr(status), _stream(stream)), "dyspec_prompt_attention")
 
 
+# dyspec_append_t, packed by hand: ctypes takes 6 us to convert as many arguments one by one, more than the kernel of a decoding step
+_APPEND_ARGS = struct.Struct("=6Q5q7Q10i")
+
+
 def dyspec_append_kv_paged(k_new, v_new, q, q_out, k_cache, v_cache, kv_total_rows: int, token_offsets, context_len, depths,
                            tree_row_offset, page_table, pages_per_req: int, page_size: int, rope_table, n_positions: int,
                            rotary_dim: int, interleaved: bool, n_tokens: int, n_req: int, n_q_heads: int, n_kv_heads: int,
@@ -436,12 +440,12 @@ def dyspec_append_kv_paged(k_new, v_new, q, q_out, k_cache, v_cache, kv_total_ro
                            status=None, stream=None) -> None:
     """New tokens' K and V into the paged cache, K and Q rotated by position (see include/dyspec.h).  Strides count
     values from one token's row to the next, 0 = packed; depths and tree_row_offset may be None."""
-    _check(lib.dyspec_append_kv_paged(_ptr(k_new), k_stride, _ptr(v_new), v_stride, _ptr(q), q_stride, _ptr(q_out), q_out_stride,
-                                      n_q_heads, _ptr(k_cache), _ptr(v_cache), int(kv_total_rows), _ptr(token_offsets),
-                                      _ptr(context_len), _ptr(depths), _ptr(tree_row_offset), n_req, n_tokens,
-                                      _ptr(page_table), int(pages_per_req), int(page_size), _ptr(rope_table), n_positions,
-                                      rotary_dim, int(bool(interleaved)), n_kv_heads, head_dim, _ptr(status),
-                                      _stream(stream)), "dyspec_append_kv_paged")
+    args = _APPEND_ARGS.pack(_ptr(k_new) or 0, _ptr(v_new) or 0, _ptr(q) or 0, _ptr(q_out) or 0, _ptr(k_cache) or 0, _ptr(v_cache) or 0,
+                             k_stride, v_stride, q_stride, q_out_stride, kv_total_rows, _ptr(token_offsets) or 0,
+                             _ptr(context_len) or 0, _ptr(depths) or 0, _ptr(tree_row_offset) or 0, _ptr(page_table) or 0,
+                             _ptr(rope_table) or 0, _ptr(status) or 0, n_req, n_tokens, n_q_heads, n_kv_heads, head_dim,
+                             pages_per_req, page_size, n_positions, rotary_dim, interleaved)
+    _check(lib.dyspec_append_kv_paged(args, _stream(stream)), "dyspec_append_kv_paged")
 
 
 def dyspec_release_cache() -> None:

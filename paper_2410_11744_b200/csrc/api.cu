@@ -47,13 +47,7 @@ cudaError_t launch_compact_kv_paged(void* k_cache, void* v_cache, const int64_t*
 cudaError_t launch_compact_kv(void* k_cache, void* v_cache, const int64_t* kv_row_offset, const int32_t* prefix_len,
                               const int32_t* accepted_nodes, const int32_t* n_accepted, int n_req, int max_out,
                               int row_bytes, int keep_root, int32_t* new_prefix_len, cudaStream_t stream);
-cudaError_t launch_append_kv_paged(const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride, const void* q,
-                                   int64_t q_stride, void* q_out, int64_t q_out_stride, int n_q_heads, void* k_cache,
-                                   void* v_cache, int64_t cache_rows, const int32_t* token_offsets,
-                                   const int32_t* context_len, const int32_t* depths, const int64_t* tree_row_offset,
-                                   int n_req, int n_tokens, const int32_t* page_table, int pages_per_req, int page_shift,
-                                   const float* rope_table, int n_positions, int rotary_dim, int interleaved,
-                                   int n_kv_heads, int head_dim, int32_t* status, cudaStream_t stream);
+cudaError_t launch_append_kv_paged(const dyspec_append_t& a, int page_shift, cudaStream_t stream);
 cudaError_t launch_attn_small(int head_dim, int n_ctas, const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv,
                             const AttnParams& p, const WorkItem* host_items, bool early_start, cudaStream_t stream);
 cudaError_t launch_attn_causal(int head_dim, int n_ctas, const CUtensorMap& mq, const CUtensorMap& mk, const CUtensorMap& mv,
@@ -217,6 +211,7 @@ struct dyspec_plan {
   bool allow_queue = true;              // false: fixed lists only (callers that cannot provide zeroed queue words)
   size_t queue_offset = 0;              // dynamic plans: byte offset of the two queue words inside the caller's workspace
   size_t counters_offset = 0;           // plans with split groups: byte offset of the groups' counter pairs in the workspace
+  bool merge_last = false;              // causal plans, small tiles: a group's pieces are merged by the one that finishes last
   bool merge_in_kernel = false;         // tensor-core regime: split groups are merged by their own items, no combine launch
   int cluster_fit[9] = {-1, -1, -1, -1, -1, -1, -1, -1, -1};   // clusters of C CTAs of the regime's kernel the device holds at once (-1: not known)
   std::vector<WorkItem> items_queue;    // dynamic plans: all items in queue order
@@ -229,7 +224,8 @@ namespace {
 // and deal them to CTAs so that every CTA gets about the same number of key tiles (plus a fixed
 // per-item cost for the Q load and the epilogue).  A group that ends up in several items is a
 // split-KV group: its items write fp32 partials that the combine step merges.
-void schedule(dyspec_plan& pl) {
+// chosen_cluster: a causal plan's cluster size, set already (0: chosen here).
+void schedule(dyspec_plan& pl, int chosen_cluster = 0) {
   const int bm = pl.bm, bn = pl.bn, g = pl.g;
   const int nodes_per_tile = bm / g;
   struct Group { int req, kvh, row0, tiles; };
@@ -269,10 +265,10 @@ void schedule(dyspec_plan& pl) {
   // Cluster mode (warp-level regime): when every group can be cut into the same number C of pieces
   // and all pieces fit in one wave, launch one cluster of C CTAs per group; the pieces are merged
   // through distributed shared memory instead of a round trip through global memory.
-  pl.cluster = 1;
+  if (chosen_cluster == 0) pl.cluster = 1;
   const Tuning& tn = pl.tune;
   const int kNumSMs = pl.n_sms;
-  if (pl.regime == 0 && tn.combine_mode == 2 && tn.force_ctas <= 0) {
+  if (chosen_cluster == 0 && pl.regime == 0 && tn.combine_mode == 2 && tn.force_ctas <= 0) {
     int max_tiles = 0;
     for (const Group& gr : groups) max_tiles = std::max(max_tiles, gr.tiles);
     const double mean_tiles = double(total_tiles) / double(groups.size());
@@ -633,67 +629,130 @@ void schedule(dyspec_plan& pl) {
   }
 }
 
-// Scheduler of the causal kernel (tensor-core regime of chunk and prompt plans).  The groups, (request, kv head, tile of 256
-// packed rows), differ in length -- a row sees the keys in front of it -- so CTAs take work items from one queue, longest
-// first.  Groups longer than what a CTA should take are cut into pieces of equal length, whose partials the combine
-// launch merges: how long a piece may be is the candidate with the smallest makespan of the queue.  Costs in units of one
-// key tile of both query halves (1.3 us): kOneHalf of it when 128 rows or fewer are live, kItemCost per item (Q, pipeline
-// fill, output), kPartialCost per piece (fp32 rows instead of bf16), kCombineCost for the launch behind the kernel.
-void schedule_causal(dyspec_plan& pl) {
-  constexpr double kOneHalf = 0.7, kItemCost = 2.0, kPartialCost = 1.0, kCombineCost = 3.0;
+// Scheduler of causal attention (chunk and prompt plans).  The groups, (request, kv head, query tile), differ in length -- a
+// row sees the keys in front of it.  Groups longer than what a CTA should take are cut into pieces of equal length whose
+// partials are merged: how long a piece may be is the candidate with the smallest makespan, pieces taken longest first by
+// the CTA that is free first.  The causal tensor-core kernel's CTAs do that on the device (a queue); the small-tile kernel's
+// get the lists that it gives.
+// Costs are in key tiles (tensor cores: 128 keys, both query halves, 1.7 us; small tiles: 64 keys, 0.75 us with all SMs
+// streaming), found by taking measured calls apart.
+struct CausalCosts {
+  double one_half;        // a tile when 128 rows or fewer are live (tensor cores)
+  double item;            // Q, pipeline fill, output
+  double partial;         // a piece: fp32 rows instead of bf16
+  double merge_last;      // merged by the last piece to finish
+  double merge_launch;    // merged by the combine launch
+};
+constexpr CausalCosts kCausalTc{0.7, 2.0, 1.0, 0.0, 3.0}, kCausalSmall{1.0, 3.0, 1.0, 3.0, 8.0};
+
+// Pieces of few rows are merged by whichever finishes last (small-tile kernel): a warp per row, all pieces' values requested at
+// once, 2 us for 18 pieces of 8 rows where a launch behind the kernel takes 4 - 5.  64 rows would be 600 KB through one SM.
+constexpr int kMergeLastRows = 16;
+
+void schedule_causal(dyspec_plan& pl, int64_t max_rows) {
+  const bool tc = pl.regime == 1;
+  const CausalCosts& cost = tc ? kCausalTc : kCausalSmall;
   struct Group { int req, kvh, row0, tiles; double unit; };
   std::vector<Group> groups;
   pl.total_tiles = 0;
   const int nodes_per_tile = pl.bm / pl.g;
+  int longest = 0;
+  double most = 0, total = 0;                              // cost of the longest group, of all
   for (int r = 0; r < pl.n_req; ++r) {
     const ReqInfo& rq = pl.reqs[size_t(r)];
     for (int64_t n0 = 0; n0 < rq.n_nodes; n0 += nodes_per_tile) {
       const int64_t end = std::min<int64_t>(rq.n_nodes, n0 + nodes_per_tile);
       const int tiles = int((int64_t(rq.prefix_len) + end + pl.bn - 1) / pl.bn);
-      const double unit = (end - n0) * pl.g > pl.bm / 2 ? 1.0 : kOneHalf;
+      const double unit = (end - n0) * pl.g > pl.bm / 2 ? 1.0 : cost.one_half;
       for (int kvh = 0; kvh < pl.hkv; ++kvh) groups.push_back({r, kvh, int(n0 * pl.g), tiles, unit});
       pl.total_tiles += int64_t(tiles) * pl.hkv;
+      longest = std::max(longest, tiles);
+      most = std::max(most, tiles * unit + cost.item);
+      total += (tiles * unit + cost.item) * pl.hkv;
     }
   }
   pl.n_groups = int64_t(groups.size());
   pl.items.clear(); pl.cta_begin.assign(1, 0); pl.split_groups.clear(); pl.items_queue.clear(); pl.items_strided.clear();
   pl.n_slots = 0; pl.max_splits = 1; pl.items_stride = 1; pl.cluster = 1; pl.dynamic = false; pl.n_ctas = 0;
+  pl.merge_last = !tc && max_rows <= kMergeLastRows && pl.tune.combine_mode != 0;
   if (groups.empty()) return;
-  const int n_sms = pl.tune.force_ctas > 0 ? pl.tune.force_ctas : pl.n_sms;
-  auto pieces_of = [&](const Group& gr, int longest) { return (gr.tiles + longest - 1) / longest; };
-  // makespan of the queue, the pieces taken longest first by the CTA that is free first
-  std::vector<double> costs, heap;
-  auto makespan = [&](int longest) {
-    costs.clear();
+  const int n_sms = pl.tune.force_ctas > 0 ? std::min(pl.tune.force_ctas, 0xffff) : pl.n_sms;
+  const double merge = pl.merge_last ? cost.merge_last : cost.merge_launch;
+  // Small tiles are bound by the stream of K and V: fewer CTAs than SMs leave each a larger share of the memory, up to 1 / 0.85.
+  auto rate = [&](int64_t n_ctas) { return tc ? 1.0 : std::min(1.0, std::max(0.85, double(n_ctas) / n_sms)); };
+  auto pieces_of = [&](const Group& gr, int len) { return (gr.tiles + len - 1) / len; };
+  // makespan, and which CTA takes which piece (in the order of the pieces that the loop below makes)
+  std::vector<uint64_t> pieces, heap;                      // cost in 1/64 tiles and ~number of a piece; load and number of a CTA
+  auto deal = [&](int len, std::vector<int>& owner) {
+    pieces.clear();
     bool split = false;
     for (const Group& gr : groups) {
-      const int n = pieces_of(gr, longest);
+      const int n = pieces_of(gr, len);
       split = split || n > 1;
-      for (int c = 0; c < n; ++c)
-        costs.push_back(gr.unit * double(int64_t(gr.tiles) * (c + 1) / n - int64_t(gr.tiles) * c / n) + kItemCost + (n > 1 ? kPartialCost : 0.0));
+      for (int c = 0; c < n; ++c) {
+        const double x = gr.unit * double(int64_t(gr.tiles) * (c + 1) / n - int64_t(gr.tiles) * c / n) + cost.item + (n > 1 ? cost.partial : 0.0);
+        pieces.push_back(uint64_t(x * 64.0) << 24 | uint64_t(0xffffffu - pieces.size()));
+      }
     }
-    std::sort(costs.begin(), costs.end(), std::greater<double>());
-    heap.assign(size_t(n_sms), 0.0);                       // a heap of equal values is one
-    for (double c : costs) {
-      std::pop_heap(heap.begin(), heap.end(), std::greater<double>());
-      heap.back() += c;
-      std::push_heap(heap.begin(), heap.end(), std::greater<double>());
+    std::sort(pieces.begin(), pieces.end(), std::greater<uint64_t>());
+    heap.clear();
+    for (int c = 0; c < n_sms; ++c) heap.push_back(uint64_t(c));                     // (sorted: a heap)
+    owner.resize(pieces.size());
+    uint64_t most_loaded = 0;
+    for (const uint64_t pc : pieces) {
+      std::pop_heap(heap.begin(), heap.end(), std::greater<uint64_t>());
+      uint64_t& cta = heap.back();
+      owner[size_t(0xffffffu - (pc & 0xffffffu))] = int(cta & 0xffffu);
+      cta += pc >> 24 << 16;
+      most_loaded = std::max(most_loaded, cta >> 16);
+      std::push_heap(heap.begin(), heap.end(), std::greater<uint64_t>());
     }
-    return *std::max_element(heap.begin(), heap.end()) + (split ? kCombineCost : 0.0);
+    const double last = double(most_loaded) / 64.0;
+    return last * rate(int64_t(pieces.size())) + (split ? merge : 0.0);
   };
-  int longest = 0;
-  for (const Group& gr : groups) longest = std::max(longest, gr.tiles);
-  if (pl.n_groups < 8 * int64_t(n_sms) && pl.tune.whole_groups != 2) {     // (with more, the queue's tail is short whatever the pieces)
-    const int whole = longest;
-    double best = makespan(whole);
-    for (int per_sm = 1; per_sm <= 4; ++per_sm) {
-      const int64_t share = (pl.total_tiles + int64_t(n_sms) * per_sm - 1) / (int64_t(n_sms) * per_sm);
-      for (int64_t len : {share, share + 1, share + share / 4 + 1}) {
-        if (len < 2 || len >= whole) continue;
-        if (const double cost = makespan(int(len)); cost < best) { best = cost; longest = int(len); }
+  std::vector<int> owner, trial;
+  const int whole = longest;
+  if (pl.n_groups < 8 * int64_t(n_sms) && pl.tune.whole_groups != 2) {     // (with more, the tail is short whatever the pieces)
+    // Candidates by what they can reach at best; one that cannot beat the best makespan so far by 2 % ends the search.
+    struct Candidate { double bound; int len; };
+    std::vector<Candidate> order{{std::max(most, total / n_sms) * rate(pl.n_groups), whole}};
+    const double share = double(pl.total_tiles) / n_sms;
+    for (double x : {0.25, 0.34, 0.5, 0.67, 0.75, 0.9, 1.0, 1.05, 1.1, 1.25, 1.5, 2.0, 3.0}) {
+      const int len = std::max(2, int(std::ceil(share * x)));
+      if (len >= whole || order.back().len == len) continue;
+      double sum = 0, piece = 0;
+      int64_t n_pieces = 0;
+      for (const Group& gr : groups) {
+        const int n = pieces_of(gr, len);
+        n_pieces += n;
+        sum += gr.unit * gr.tiles + n * (cost.item + (n > 1 ? cost.partial : 0.0));
+        piece = std::max(piece, gr.unit * ((gr.tiles + n - 1) / n) + cost.item + (n > 1 ? cost.partial : 0.0));
+      }
+      order.push_back({std::max(piece, sum / n_sms) * rate(n_pieces) + merge, len});
+    }
+    std::stable_sort(order.begin(), order.end(), [](const Candidate& a, const Candidate& b) { return a.bound < b.bound; });
+    double best = 0;
+    for (const Candidate& c : order) {
+      if (!owner.empty() && c.bound >= 0.98 * best) break;
+      if (const double cost_now = deal(c.len, trial); owner.empty() || cost_now < best) { best = cost_now; longest = c.len; owner.swap(trial); }
+    }
+    // Small tiles: one thread-block cluster per group, merged on chip, where all clusters run at once and the groups are alike.
+    // Its merge is the cheapest, but a CTA that merges keeps two of its six ring stages free for it and streams more
+    // slowly: one token over 1024 keys, 32 groups, 11.0 us against 11.8; over 16384, 32 groups, 55.8 against 50.2.
+    if (!tc && pl.tune.combine_mode == 2 && pl.tune.force_ctas <= 0) {
+      const double mean = double(pl.total_tiles) / double(groups.size());
+      int least = whole;
+      for (const Group& gr : groups) least = std::min(least, gr.tiles);
+      for (int C : {8, 4, 2}) {
+        if (pl.n_groups * C > n_sms || least < 2 * C || whole > 1.3 * mean) continue;
+        if (pl.cluster_fit[C] >= 0 && pl.n_groups > pl.cluster_fit[C]) continue;
+        if (std::max(0.92, 1.3 * double(pl.n_groups) * C / n_sms) * ((whole + C - 1) / C) + cost.item + 1.5 < best) pl.cluster = C;
+        break;
       }
     }
   }
+  if (pl.cluster > 1) return;                              // (laid out by schedule)
+  if (!tc && owner.empty()) deal(longest, owner);
   for (const Group& gr : groups) {
     const ReqInfo& rq = pl.reqs[size_t(gr.req)];
     const int n = pieces_of(gr, longest);
@@ -716,11 +775,26 @@ void schedule_causal(dyspec_plan& pl) {
       pl.max_splits = std::max(pl.max_splits, n);
     }
   }
-  std::stable_sort(pl.items.begin(), pl.items.end(),
-                   [](const WorkItem& a, const WorkItem& b) { return a.tile_end - a.tile_begin > b.tile_end - b.tile_begin; });
+  pl.merge_last = pl.merge_last && !pl.split_groups.empty();
+  const auto longer = [](const WorkItem& a, const WorkItem& b) { return a.tile_end - a.tile_begin > b.tile_end - b.tile_begin; };
   pl.n_ctas = int(std::min<int64_t>(int64_t(pl.items.size()), n_sms));
-  pl.dynamic = int64_t(pl.items.size()) > pl.n_ctas;
-  pl.items_strided = pl.items;
+  if (tc) {
+    std::stable_sort(pl.items.begin(), pl.items.end(), longer);
+    pl.dynamic = int64_t(pl.items.size()) > pl.n_ctas;
+    pl.items_strided = pl.items;
+    return;
+  }
+  std::vector<std::vector<WorkItem>> lists{size_t(pl.n_ctas)};
+  for (size_t i = 0; i < pl.items.size(); ++i) lists[size_t(owner[i])].push_back(pl.items[i]);
+  for (std::vector<WorkItem>& list : lists) {
+    std::stable_sort(list.begin(), list.end(), longer);
+    pl.items_stride = std::max(pl.items_stride, int(list.size()));
+  }
+  pl.items_strided.assign(size_t(pl.n_ctas) * size_t(pl.items_stride), WorkItem{});
+  for (size_t c = 0; c < lists.size(); ++c) {
+    std::copy(lists[c].begin(), lists[c].end(), pl.items_strided.begin() + ptrdiff_t(c * size_t(pl.items_stride)));
+    pl.items_strided[c * size_t(pl.items_stride)].n_in_cta = int(lists[c].size());
+  }
 }
 
 // Device memory of the plans' tables.  A serving loop makes a plan for every step, and cudaMalloc, cudaFree (which waits
@@ -1094,37 +1168,32 @@ static bool row_stride(int64_t* stride, int64_t row_values) {
   return *stride >= row_values && (*stride & 7) == 0 && *stride < (int64_t(1) << 38);   // (2^39 bytes: a tensor map's limit is 2^40)
 }
 
-int dyspec_append_kv_paged(const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride, const void* q,
-                           int64_t q_stride, void* q_out, int64_t q_out_stride, int n_q_heads, void* k_cache, void* v_cache,
-                           int64_t kv_total_rows, const int32_t* token_offsets, const int32_t* context_len,
-                           const int32_t* depths, const int64_t* tree_row_offset, int n_req, int n_tokens,
-                           const int32_t* page_table, int pages_per_req, int page_size, const float* rope_table,
-                           int n_positions, int rotary_dim, int interleaved, int n_kv_heads, int head_dim, int32_t* status,
-                           dyspec_stream_t stream) {
-  if (n_q_heads < 0 || n_kv_heads <= 0 || n_req < 0 || n_tokens < 0 || kv_total_rows < 0 || n_positions < 0 || rotary_dim < 0)
+static_assert(sizeof(dyspec_append_t) == 184, "18 words of 8 bytes, 10 of 4, no gaps: bindings pack it by hand");
+int dyspec_append_kv_paged(const dyspec_append_t* args, dyspec_stream_t stream) {
+  if (!args) return DYSPEC_ERR_INVALID_ARG;
+  dyspec_append_t a = *args;
+  if (a.n_q_heads < 0 || a.n_kv_heads <= 0 || a.n_req < 0 || a.n_tokens < 0 || a.kv_total_rows < 0 || a.n_positions < 0 || a.rotary_dim < 0)
     return DYSPEC_ERR_INVALID_ARG;
-  if (!(head_dim == 64 || head_dim == 128) || n_q_heads > (1 << 16) || n_kv_heads > (1 << 16)) return DYSPEC_ERR_UNSUPPORTED;
-  if (rotary_dim % 16 != 0) return DYSPEC_ERR_UNSUPPORTED;
-  if (rotary_dim > head_dim) return DYSPEC_ERR_INVALID_ARG;
-  if (!tree_row_offset && (pages_per_req <= 0 || page_size <= 0 || (page_size & (page_size - 1)))) return DYSPEC_ERR_INVALID_ARG;
-  const int64_t q_row = int64_t(n_q_heads) * head_dim, kv_row = int64_t(n_kv_heads) * head_dim;
-  if (!row_stride(&k_stride, kv_row) || !row_stride(&v_stride, kv_row) || !row_stride(&q_stride, q_row) || !row_stride(&q_out_stride, q_row))
+  if (!(a.head_dim == 64 || a.head_dim == 128) || a.n_q_heads > (1 << 16) || a.n_kv_heads > (1 << 16)) return DYSPEC_ERR_UNSUPPORTED;
+  if (a.rotary_dim % 16 != 0) return DYSPEC_ERR_UNSUPPORTED;
+  if (a.rotary_dim > a.head_dim) return DYSPEC_ERR_INVALID_ARG;
+  const bool in_pages = a.tree_row_offset == nullptr;
+  if (in_pages && (a.pages_per_req <= 0 || a.page_size <= 0 || (a.page_size & (a.page_size - 1)))) return DYSPEC_ERR_INVALID_ARG;
+  const int64_t q_row = int64_t(a.n_q_heads) * a.head_dim, kv_row = int64_t(a.n_kv_heads) * a.head_dim;
+  if (!row_stride(&a.k_stride, kv_row) || !row_stride(&a.v_stride, kv_row) || !row_stride(&a.q_stride, q_row) || !row_stride(&a.q_out_stride, q_row))
     return DYSPEC_ERR_INVALID_ARG;
-  if (n_req == 0 || n_tokens == 0) return DYSPEC_OK;
-  if (!k_new || !v_new || !k_cache || !v_cache || !token_offsets || !context_len || (!tree_row_offset && !page_table))
+  if (a.n_req == 0 || a.n_tokens == 0) return DYSPEC_OK;
+  if (!a.k_new || !a.v_new || !a.k_cache || !a.v_cache || !a.token_offsets || !a.context_len || (in_pages && !a.page_table))
     return DYSPEC_ERR_INVALID_ARG;
-  if (n_q_heads > 0 && (!q || !q_out || !aligned(q, 16) || !aligned(q_out, 16) || (q == q_out && q_stride != q_out_stride)))
+  if (a.n_q_heads > 0 && (!a.q || !a.q_out || !aligned(a.q, 16) || !aligned(a.q_out, 16) || (a.q == a.q_out && a.q_stride != a.q_out_stride)))
     return DYSPEC_ERR_INVALID_ARG;
-  if (rotary_dim > 0 && (!rope_table || !aligned(rope_table, 16))) return DYSPEC_ERR_INVALID_ARG;
-  if (!aligned(k_new, 16) || !aligned(v_new, 16) || !aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(token_offsets, 4) ||
-      !aligned(context_len, 4) || !aligned(depths, 4) || !aligned(tree_row_offset, 8) || !aligned(page_table, 4) || !aligned(status, 4))
+  if (a.rotary_dim > 0 && (!a.rope_table || !aligned(a.rope_table, 16))) return DYSPEC_ERR_INVALID_ARG;
+  if (!aligned(a.k_new, 16) || !aligned(a.v_new, 16) || !aligned(a.k_cache, 16) || !aligned(a.v_cache, 16) || !aligned(a.token_offsets, 4) ||
+      !aligned(a.context_len, 4) || !aligned(a.depths, 4) || !aligned(a.tree_row_offset, 8) || !aligned(a.page_table, 4) || !aligned(a.status, 4))
     return DYSPEC_ERR_INVALID_ARG;
   int shift = 0;
-  while (!tree_row_offset && (int64_t(1) << shift) < page_size) ++shift;
-  cudaError_t e = launch_append_kv_paged(k_new, k_stride, v_new, v_stride, q, q_stride, q_out, q_out_stride, n_q_heads, k_cache,
-                                         v_cache, kv_total_rows, token_offsets, context_len, depths, tree_row_offset, n_req,
-                                         n_tokens, page_table, pages_per_req, shift, rope_table, n_positions, rotary_dim,
-                                         interleaved != 0, n_kv_heads, head_dim, status, reinterpret_cast<cudaStream_t>(stream));
+  while (in_pages && (int64_t(1) << shift) < a.page_size) ++shift;
+  cudaError_t e = launch_append_kv_paged(a, shift, reinterpret_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? DYSPEC_OK : cuda_failed(e, "append launch");
 }
 
@@ -1140,9 +1209,10 @@ static void finish_host_plan(dyspec_plan* pl, int64_t max_rows) {
   if (pl->tune.combine_mode == 2)
     for (int C : {2, 4, 8})
       pl->cluster_fit[C] = pl->regime == 1 ? attn_tc_max_clusters(pl->d, C) : attn_small_max_clusters(pl->d, C);
-  if (pl->kind != PlanKind::kTree && pl->regime == 1) {
-    pl->tune.combine_mode = 0;            // the causal kernel's partials are merged by the combine launch
-    schedule_causal(*pl);
+  if (pl->kind != PlanKind::kTree) {
+    if (pl->regime == 1) pl->tune.combine_mode = 0;        // the causal kernel's partials are merged by the combine launch
+    schedule_causal(*pl, max_rows);
+    if (pl->cluster > 1) schedule(*pl, pl->cluster);
   } else {
     schedule(*pl);
   }
@@ -1165,7 +1235,7 @@ static void finish_host_plan(dyspec_plan* pl, int64_t max_rows) {
     pl->workspace_bytes = pl->counters_offset + ((pl->split_groups.size() * 2 * sizeof(int32_t) + 255) & ~size_t(255));
     // (the items of a group wait for each other inside the kernel: only when every CTA of the launch is
     //  resident at once, i.e. one CTA per SM and no more CTAs than SMs; a forced larger grid keeps the combine launch)
-    pl->merge_in_kernel = pl->regime == 1 && pl->tune.combine_mode != 0 && pl->n_ctas <= pl->n_sms;
+    pl->merge_in_kernel = pl->merge_last || (pl->regime == 1 && pl->tune.combine_mode != 0 && pl->n_ctas <= pl->n_sms);
   }
   if (pl->dynamic) {                    // the queue words follow the partials (there are none in such a plan today)
     pl->queue_offset = (pl->workspace_bytes + 255) & ~size_t(255);

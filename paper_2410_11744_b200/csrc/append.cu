@@ -10,6 +10,7 @@
 // thread and Q may be rotated in place.  A head has D / 16 units, a power of two, so a thread meets the same unit of
 // every head that it works on: its 16 cosines and sines stay in registers.  A thread asks for its chunks before it knows
 // where they go; the chain in front of the writes (request of the token, context, page) runs under those loads.
+// A token is worked on by a group of 32 to 256 threads, as many as leave each about kBatch units.
 #include "common.cuh"
 
 namespace dyspec {
@@ -29,7 +30,8 @@ struct AppendParams {
   const float* rope;
   int32_t* status;
   int64_t cache_rows;
-  int n_req, pages_per_req, page_shift, n_positions, rot, interleaved, hq, hkv;
+  int n_req, n_tokens, pages_per_req, page_shift, n_positions, rot, interleaved, hq, hkv;
+  int log2_group;                         // threads per token
 };
 
 // The request that owns `token`: how many requests end at or before it (n_req: none, the token is padding).  Whole
@@ -54,7 +56,10 @@ template <int D>
 __global__ void __launch_bounds__(kThreads) append_kv_kernel(const AppendParams p) {
   constexpr int P = D / 16;               // units per head
   constexpr int C = D / 8;                // 16-byte chunks per head
-  const int token = blockIdx.x;
+  const int group = 1 << p.log2_group, in_group = int(threadIdx.x) & (group - 1);
+  const int64_t token64 = int64_t(blockIdx.x) * (kThreads >> p.log2_group) + (threadIdx.x >> p.log2_group);
+  if (token64 >= p.n_tokens) return;      // (a group is whole warps)
+  const int token = int(token64);
   const int lane = threadIdx.x & 31;
   const int pair_units = p.rot >> 4;
   const int u = threadIdx.x % P;          // the same unit of every head (kThreads is a multiple of P)
@@ -62,7 +67,7 @@ __global__ void __launch_bounds__(kThreads) append_kv_kernel(const AppendParams 
   const int c0 = turned && !p.interleaved ? u : 2 * u;
   const int c1 = turned && !p.interleaved ? u + pair_units : 2 * u + 1;
   const int n_heads = p.hq + 2 * p.hkv;
-  const int head0 = blockIdx.y * (kThreads / P) + threadIdx.x / P, head_step = gridDim.y * (kThreads / P);
+  const int head0 = blockIdx.y * (group / P) + in_group / P, head_step = gridDim.y * (group / P);
 
   uint4 a[kBatch], b[kBatch];
   auto fetch = [&](int i, int head) {
@@ -92,7 +97,7 @@ __global__ void __launch_bounds__(kThreads) append_kv_kernel(const AppendParams 
   }
   // a token without a row or a rotation is left out whole (the checks hold for every thread of the token alike)
   if (j < 0 || row < 0 || row >= p.cache_rows || (p.rot > 0 && (position < 0 || position >= p.n_positions))) {
-    if (p.status && threadIdx.x == 0 && blockIdx.y == 0) atomicCAS(p.status, 0, DYSPEC_ERR_INVALID_ARG);
+    if (p.status && in_group == 0 && blockIdx.y == 0) atomicCAS(p.status, 0, DYSPEC_ERR_INVALID_ARG);
     return;
   }
   float cs[8], sn[8];
@@ -146,26 +151,24 @@ __global__ void __launch_bounds__(kThreads) append_kv_kernel(const AppendParams 
 
 }  // namespace
 
-cudaError_t launch_append_kv_paged(const void* k_new, int64_t k_stride, const void* v_new, int64_t v_stride, const void* q,
-                                   int64_t q_stride, void* q_out, int64_t q_out_stride, int n_q_heads, void* k_cache,
-                                   void* v_cache, int64_t cache_rows, const int32_t* token_offsets,
-                                   const int32_t* context_len, const int32_t* depths, const int64_t* tree_row_offset,
-                                   int n_req, int n_tokens, const int32_t* page_table, int pages_per_req, int page_shift,
-                                   const float* rope_table, int n_positions, int rotary_dim, int interleaved,
-                                   int n_kv_heads, int head_dim, int32_t* status, cudaStream_t stream) {
+cudaError_t launch_append_kv_paged(const dyspec_append_t& a, int page_shift, cudaStream_t stream) {
   AppendParams p{};
-  p.q = static_cast<const uint4*>(q); p.k = static_cast<const uint4*>(k_new); p.v = static_cast<const uint4*>(v_new);
-  p.q_out = static_cast<uint4*>(q_out); p.k_cache = static_cast<uint4*>(k_cache); p.v_cache = static_cast<uint4*>(v_cache);
-  p.q_stride = q_stride / 8; p.k_stride = k_stride / 8; p.v_stride = v_stride / 8; p.q_out_stride = q_out_stride / 8;
-  p.offsets = token_offsets; p.context = context_len; p.depths = depths; p.tree_row_offset = tree_row_offset;
-  p.page_table = page_table; p.rope = rope_table; p.status = status; p.cache_rows = cache_rows;
-  p.n_req = n_req; p.pages_per_req = pages_per_req; p.page_shift = page_shift; p.n_positions = n_positions;
-  p.rot = rotary_dim; p.interleaved = interleaved; p.hq = n_q_heads; p.hkv = n_kv_heads;
-  // One CTA per token, all of its heads; few tokens (less than a wave) are spread over more CTAs, one unit a thread.
-  const int heads_per_pass = kThreads / (head_dim / 16);
-  const int passes = (n_q_heads + 2 * n_kv_heads + heads_per_pass - 1) / heads_per_pass;
-  const dim3 grid(unsigned(n_tokens), unsigned(n_tokens <= kDefaultSMs ? passes : 1));
-  if (head_dim == 128) append_kv_kernel<128><<<grid, kThreads, 0, stream>>>(p);
+  p.q = static_cast<const uint4*>(a.q); p.k = static_cast<const uint4*>(a.k_new); p.v = static_cast<const uint4*>(a.v_new);
+  p.q_out = static_cast<uint4*>(a.q_out); p.k_cache = static_cast<uint4*>(a.k_cache); p.v_cache = static_cast<uint4*>(a.v_cache);
+  p.q_stride = a.q_stride / 8; p.k_stride = a.k_stride / 8; p.v_stride = a.v_stride / 8; p.q_out_stride = a.q_out_stride / 8;
+  p.offsets = a.token_offsets; p.context = a.context_len; p.depths = a.depths; p.tree_row_offset = a.tree_row_offset;
+  p.page_table = a.page_table; p.rope = a.rope_table; p.status = a.status; p.cache_rows = a.kv_total_rows;
+  p.n_req = a.n_req; p.n_tokens = a.n_tokens; p.pages_per_req = a.pages_per_req; p.page_shift = page_shift;
+  p.n_positions = a.n_positions; p.rot = a.rotary_dim; p.interleaved = a.interleaved != 0; p.hq = a.n_q_heads; p.hkv = a.n_kv_heads;
+  // Few tokens (less than a wave of CTAs): 256 threads each and more than one CTA, one unit a thread.  Else the smallest group
+  // that needs one batch.
+  const int units = (a.n_q_heads + 2 * a.n_kv_heads) * (a.head_dim / 16);
+  const bool few = a.n_tokens <= kDefaultSMs;
+  p.log2_group = 5;
+  while (p.log2_group < 8 && (few || units > (kBatch << p.log2_group))) ++p.log2_group;
+  const int per_cta = kThreads >> p.log2_group;
+  const dim3 grid(unsigned((int64_t(a.n_tokens) + per_cta - 1) / per_cta), unsigned(few ? (units + kThreads - 1) / kThreads : 1));
+  if (a.head_dim == 128) append_kv_kernel<128><<<grid, kThreads, 0, stream>>>(p);
   else append_kv_kernel<64><<<grid, kThreads, 0, stream>>>(p);
   return cudaGetLastError();
 }

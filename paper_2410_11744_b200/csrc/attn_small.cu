@@ -144,6 +144,58 @@ __device__ __forceinline__ void tmem_st_rows(uint32_t taddr, const float (&v)[NJ
       : "memory");
 }
 
+// One row of a split group, by one warp: out = (sum_s w_s O_s) / (sum_s w_s l_s), w_s = 2^(m_s - max m).  Every lane holds
+// the pieces' maxima and sums 32 pieces at a time, and D / 32 columns; four pieces' columns are in flight.
+template <int D>
+__device__ __noinline__ void merge_row(const float* base, int slot_floats, int n_splits, int rr, __nv_bfloat16* out) {
+  constexpr int V = D / 32;
+  const int lane = threadIdx.x & 31;
+  float m = -INFINITY;
+  for (int s = lane; s < n_splits; s += 32) m = fmaxf(m, ld_cg_f32(base + size_t(s) * slot_floats + BM * D + rr));
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  const float ref = m == -INFINITY ? 0.f : m;
+  float acc[V], l = 0.f;
+#pragma unroll
+  for (int e = 0; e < V; ++e) acc[e] = 0.f;
+  for (int s0 = 0; s0 < n_splits; s0 += 32) {
+    float w = 0.f;
+    if (s0 + lane < n_splits) {
+      const float* at = base + size_t(s0 + lane) * slot_floats + BM * D + rr;
+      w = fast_exp2(ld_cg_f32(at) - ref);
+      l += w * ld_cg_f32(at + BM);
+    }
+    const int here = min(32, n_splits - s0);
+    for (int s1 = 0; s1 < here; s1 += 4) {
+      float v[4][V];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float* at = base + size_t(s0 + min(s1 + k, here - 1)) * slot_floats + rr * D + lane * V;
+        if constexpr (V == 4) {
+          const float4 x = ld_cg_f32x4(at);
+          v[k][0] = x.x; v[k][1] = x.y; v[k][2] = x.z; v[k][3] = x.w;
+        } else {
+          const float2 x = ld_cg_f32x2(at);
+          v[k][0] = x.x; v[k][1] = x.y;
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float wk = __shfl_sync(0xffffffffu, w, s1 + k);       // (0 behind the last piece)
+        if (s1 + k < here) {
+#pragma unroll
+          for (int e = 0; e < V; ++e) acc[e] += wk * v[k][e];
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+  const float inv = l > 0.f ? 1.f / l : 0.f;
+  if constexpr (V == 4) *reinterpret_cast<uint2*>(out + lane * 4) = make_uint2(pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv));
+  else *reinterpret_cast<uint32_t*>(out + lane * 2) = pack_bf16x2(acc[0] * inv, acc[1] * inv);
+}
+
 }  // namespace
 
 // kCausal: causal attention of new tokens (a chunk over its cache, a packed prompt) instead of a tree: node i is token
@@ -840,6 +892,29 @@ tree_attn_small_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
       if (tig == 0 && set == 0) {
         if (ok_lo) { slot[BM * D + r_lo] = m_lo; slot[BM * D + BM + r_lo] = l_lo; }
         if (ok_hi) { slot[BM * D + r_hi] = m_hi; slot[BM * D + BM + r_hi] = l_hi; }
+      }
+      if (kCausal && p.merge_in_kernel) {
+        // Few rows: the piece of the group that finishes last merges them all.  Nobody waits: every piece publishes its rows
+        // (written, fenced, counted), and the one that counts up to n_splits reads them, always in the order of the pieces.
+        constexpr int kTid = kSets * kComputeWarps * 32;
+        int* last_here = reinterpret_cast<int*>(exch_ml);  // (read out above by everybody; written again behind the next barrier)
+        __threadfence();
+        asm volatile("bar.sync 1, %0;" ::"n"(kTid) : "memory");
+        if (threadIdx.x == 0) {
+          const bool last = atomicAdd(p.counters + 2 * item.group, 1) == item.n_splits - 1;
+          if (last) p.counters[2 * item.group] = 0;        // for the next launch
+          *last_here = last ? 1 : 0;
+          __threadfence();
+        }
+        asm volatile("bar.sync 1, %0;" ::"n"(kTid) : "memory");
+        if (*reinterpret_cast<volatile int*>(last_here) != 0) {
+          const float* base = p.partial + size_t(item.slot0) * p.slot_floats;
+          for (int rr = warp; item.row0 + rr < n_rows && rr < BM; rr += kSets * kComputeWarps) {
+            const int row = item.row0 + rr;
+            merge_row<D>(base, p.slot_floats, item.n_splits, rr,
+                         p.out + (size_t(rq.node0 + (row >> p.log2_g)) * p.n_q_heads + item.kv_head * g + (row & (g - 1))) * D);
+          }
+        }
       }
     }
   }

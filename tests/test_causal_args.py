@@ -15,12 +15,14 @@ def lib():
 
 
 def _append(lib, **over):
+    from paper_2410_11744_b200 import binding
     a = dict(k=P, ks=0, v=P, vs=0, q=P, qs=0, qo=2 * P, qos=0, hq=8, kc=P, vc=P, rows=1024, off=P, ctx=P, dep=None, tree=None, n_req=0,
              n=0, table=P, ppr=4, page=16, rope=P, npos=100, rot=64, inter=0, hkv=2, d=64, status=None)
     a.update(over)
-    return lib.dyspec_append_kv_paged(a["k"], a["ks"], a["v"], a["vs"], a["q"], a["qs"], a["qo"], a["qos"], a["hq"], a["kc"], a["vc"],
-                                      a["rows"], a["off"], a["ctx"], a["dep"], a["tree"], a["n_req"], a["n"], a["table"], a["ppr"], a["page"],
-                                      a["rope"], a["npos"], a["rot"], a["inter"], a["hkv"], a["d"], a["status"], None)
+    z = lambda *names: [a[name] or 0 for name in names]
+    packed = binding._APPEND_ARGS.pack(*z("k", "v", "q", "qo", "kc", "vc", "ks", "vs", "qs", "qos", "rows", "off", "ctx", "dep", "tree", "table",
+                                          "rope", "status", "n_req", "n", "hq", "hkv", "d", "ppr", "page", "npos", "rot", "inter"))
+    return lib.dyspec_append_kv_paged(packed, None)
 
 
 @pytest.mark.parametrize("code,over", [
@@ -74,6 +76,7 @@ def test_chunk_plan_refusals(lib, code, over):
 
 
 def test_calls_without_a_plan(lib):
+    assert lib.dyspec_append_kv_paged(None, None) == -1
     assert lib.dyspec_chunk_attention_paged(None, P, 0, P, P, P, 4, P, None, 0, None, None) == -1
     assert lib.dyspec_prompt_attention(None, P, 0, P, 0, P, 0, P, None, 0, None, None) == -1
     assert lib.dyspec_plan_create_chunk(None, 8, 2, 64, 0, None, None, 0, 128, 0.0) == -1
