@@ -631,8 +631,9 @@ void schedule(dyspec_plan& pl, int chosen_cluster = 0) {
 
 // Scheduler of causal attention (chunk and prompt plans).  The groups, (request, kv head, query tile), differ in length -- a
 // row sees the keys in front of it.  Groups longer than what a CTA should take are cut into pieces of equal length whose
-// partials are merged: how long a piece may be is the candidate with the smallest makespan, pieces taken longest first by
-// the CTA that is free first.  The causal tensor-core kernel's CTAs do that on the device (a queue); the small-tile kernel's
+// partials are merged: all of them, or the shortest ones, which even out what whole groups leave.  How long a piece may be and
+// how many groups stay whole is the candidate with the smallest makespan, pieces taken longest first by the CTA that is free
+// first.  The causal tensor-core kernel's CTAs do that on the device (a queue); the small-tile kernel's
 // get the lists that it gives.
 // Costs are in key tiles (tensor cores: 128 keys, both query halves, 1.7 us; small tiles: 64 keys, 0.75 us with all SMs
 // streaming), found by taking measured calls apart.
@@ -672,6 +673,7 @@ void schedule_causal(dyspec_plan& pl, int64_t max_rows) {
     }
   }
   pl.n_groups = int64_t(groups.size());
+  std::stable_sort(groups.begin(), groups.end(), [](const Group& a, const Group& b) { return a.tiles * a.unit > b.tiles * b.unit; });
   pl.items.clear(); pl.cta_begin.assign(1, 0); pl.split_groups.clear(); pl.items_queue.clear(); pl.items_strided.clear();
   pl.n_slots = 0; pl.max_splits = 1; pl.items_stride = 1; pl.cluster = 1; pl.dynamic = false; pl.n_ctas = 0;
   pl.merge_last = !tc && max_rows <= kMergeLastRows && pl.tune.combine_mode != 0;
@@ -680,14 +682,15 @@ void schedule_causal(dyspec_plan& pl, int64_t max_rows) {
   const double merge = pl.merge_last ? cost.merge_last : cost.merge_launch;
   // Small tiles are bound by the stream of K and V: fewer CTAs than SMs leave each a larger share of the memory, up to 1 / 0.85.
   auto rate = [&](int64_t n_ctas) { return tc ? 1.0 : std::min(1.0, std::max(0.85, double(n_ctas) / n_sms)); };
-  auto pieces_of = [&](const Group& gr, int len) { return (gr.tiles + len - 1) / len; };
+  auto pieces_of = [&](size_t gi, size_t n_whole, int len) { return gi < n_whole ? 1 : (groups[gi].tiles + len - 1) / len; };
   // makespan, and which CTA takes which piece (in the order of the pieces that the loop below makes)
   std::vector<uint64_t> pieces, heap;                      // cost in 1/64 tiles and ~number of a piece; load and number of a CTA
-  auto deal = [&](int len, std::vector<int>& owner) {
+  auto deal = [&](size_t n_whole, int len, std::vector<int>& owner) {
     pieces.clear();
     bool split = false;
-    for (const Group& gr : groups) {
-      const int n = pieces_of(gr, len);
+    for (size_t gi = 0; gi < groups.size(); ++gi) {
+      const Group& gr = groups[gi];
+      const int n = pieces_of(gi, n_whole, len);
       split = split || n > 1;
       for (int c = 0; c < n; ++c) {
         const double x = gr.unit * double(int64_t(gr.tiles) * (c + 1) / n - int64_t(gr.tiles) * c / n) + cost.item + (n > 1 ? cost.partial : 0.0);
@@ -711,40 +714,48 @@ void schedule_causal(dyspec_plan& pl, int64_t max_rows) {
     return last * rate(int64_t(pieces.size())) + (split ? merge : 0.0);
   };
   std::vector<int> owner, trial;
+  size_t n_whole_best = groups.size();
   const int whole = longest;
   if (pl.n_groups < 8 * int64_t(n_sms) && pl.tune.whole_groups != 2) {     // (with more, the tail is short whatever the pieces)
     // Candidates by what they can reach at best; one that cannot beat the best makespan so far by 2 % ends the search.
-    struct Candidate { double bound; int len; };
-    std::vector<Candidate> order{{std::max(most, total / n_sms) * rate(pl.n_groups), whole}};
-    const double share = double(pl.total_tiles) / n_sms;
-    for (double x : {0.25, 0.34, 0.5, 0.67, 0.75, 0.9, 1.0, 1.05, 1.1, 1.25, 1.5, 2.0, 3.0}) {
-      const int len = std::max(2, int(std::ceil(share * x)));
-      if (len >= whole || order.back().len == len) continue;
-      double sum = 0, piece = 0;
-      int64_t n_pieces = 0;
-      for (const Group& gr : groups) {
-        const int n = pieces_of(gr, len);
-        n_pieces += n;
-        sum += gr.unit * gr.tiles + n * (cost.item + (n > 1 ? cost.partial : 0.0));
-        piece = std::max(piece, gr.unit * ((gr.tiles + n - 1) / n) + cost.item + (n > 1 ? cost.partial : 0.0));
+    struct Candidate { double bound; size_t n_whole; int len; };
+    std::vector<Candidate> order{{std::max(most, total / n_sms) * rate(pl.n_groups), groups.size(), whole}};
+    const size_t rounds = groups.size() / size_t(n_sms);   // whole groups that every CTA can take
+    for (size_t n_whole : {size_t(0), rounds * size_t(n_sms), (rounds > 0 ? rounds - 1 : 0) * size_t(n_sms)}) {
+      if (n_whole == groups.size() || (n_whole == 0 && order.size() > 1)) continue;
+      double share = 0;                                    // what the cut groups are for a CTA
+      for (size_t gi = n_whole; gi < groups.size(); ++gi) share += groups[gi].tiles;
+      share /= n_sms;
+      for (double x : {0.25, 0.34, 0.5, 0.67, 0.75, 0.9, 1.0, 1.05, 1.1, 1.25, 1.5, 2.0, 3.0}) {
+        const int len = std::max(2, int(std::ceil(share * x)));
+        if (len >= groups[n_whole].tiles || (order.back().n_whole == n_whole && order.back().len == len)) continue;
+        double sum = 0, piece = n_whole ? most : 0.0;
+        int64_t n_pieces = 0;
+        for (size_t gi = 0; gi < groups.size(); ++gi) {
+          const Group& gr = groups[gi];
+          const int n = pieces_of(gi, n_whole, len);
+          n_pieces += n;
+          sum += gr.unit * gr.tiles + n * (cost.item + (n > 1 ? cost.partial : 0.0));
+          if (n > 1) piece = std::max(piece, gr.unit * ((gr.tiles + n - 1) / n) + cost.item + cost.partial);
+        }
+        order.push_back({std::max(piece, sum / n_sms) * rate(n_pieces) + merge, n_whole, len});
       }
-      order.push_back({std::max(piece, sum / n_sms) * rate(n_pieces) + merge, len});
     }
     std::stable_sort(order.begin(), order.end(), [](const Candidate& a, const Candidate& b) { return a.bound < b.bound; });
     double best = 0;
     for (const Candidate& c : order) {
       if (!owner.empty() && c.bound >= 0.98 * best) break;
-      if (const double cost_now = deal(c.len, trial); owner.empty() || cost_now < best) { best = cost_now; longest = c.len; owner.swap(trial); }
+      if (const double cost_now = deal(c.n_whole, c.len, trial); owner.empty() || cost_now < best) {
+        best = cost_now; longest = c.len; n_whole_best = c.n_whole; owner.swap(trial);
+      }
     }
     // Small tiles: one thread-block cluster per group, merged on chip, where all clusters run at once and the groups are alike.
     // Its merge is the cheapest, but a CTA that merges keeps two of its six ring stages free for it and streams more
     // slowly: one token over 1024 keys, 32 groups, 11.0 us against 11.8; over 16384, 32 groups, 55.8 against 50.2.
     if (!tc && pl.tune.combine_mode == 2 && pl.tune.force_ctas <= 0) {
       const double mean = double(pl.total_tiles) / double(groups.size());
-      int least = whole;
-      for (const Group& gr : groups) least = std::min(least, gr.tiles);
       for (int C : {8, 4, 2}) {
-        if (pl.n_groups * C > n_sms || least < 2 * C || whole > 1.3 * mean) continue;
+        if (pl.n_groups * C > n_sms || groups.back().tiles < 2 * C || whole > 1.3 * mean) continue;
         if (pl.cluster_fit[C] >= 0 && pl.n_groups > pl.cluster_fit[C]) continue;
         if (std::max(0.92, 1.3 * double(pl.n_groups) * C / n_sms) * ((whole + C - 1) / C) + cost.item + 1.5 < best) pl.cluster = C;
         break;
@@ -752,10 +763,11 @@ void schedule_causal(dyspec_plan& pl, int64_t max_rows) {
     }
   }
   if (pl.cluster > 1) return;                              // (laid out by schedule)
-  if (!tc && owner.empty()) deal(longest, owner);
-  for (const Group& gr : groups) {
+  if (!tc && owner.empty()) deal(n_whole_best, longest, owner);
+  for (size_t gi = 0; gi < groups.size(); ++gi) {
+    const Group& gr = groups[gi];
     const ReqInfo& rq = pl.reqs[size_t(gr.req)];
-    const int n = pieces_of(gr, longest);
+    const int n = pieces_of(gi, n_whole_best, longest);
     for (int c = 0; c < n; ++c) {
       WorkItem it{};
       it.kv_row0 = rq.kv_row0; it.prefix_len = rq.prefix_len; it.n_nodes = rq.n_nodes; it.node0 = rq.node0;
