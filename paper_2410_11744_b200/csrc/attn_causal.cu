@@ -115,6 +115,7 @@ __device__ __forceinline__ bool elect_one() {
 #endif
 constexpr int kFirstChunks = SPLIT;          // P is handed over in two pieces: 32 * kFirstChunks keys, then the rest
 constexpr int kBarP = 1;                    // named barriers 1 .. 4: 64 keys of P are in tensor memory (half A: 1, 2; half B: 3, 4)
+constexpr int kBarTurn = 5;                 // named barriers 5, 6: half A's / half B's turn to issue
 constexpr int kPCount = BMH + 32;           // a half's softmax threads + the issuing warp
 
 }  // namespace
@@ -147,14 +148,14 @@ causal_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
       mbar_init(bar(Br::kODone + h), 1);
       mbar_init(bar(Br::kOFree + h), BMH);
     }
-    mbar_init(bar(Br::kQFree), 1);
+    mbar_init(bar(Br::kQFree), 2);
     for (int s = 0; s < kSlots; ++s) {
       mbar_init(bar(Br::kSlotFull + s), 1);
-      mbar_init(bar(Br::kSlotEmpty + s), 1);
+      mbar_init(bar(Br::kSlotEmpty + s), 2);
     }
     for (int e = 0; e < 8; ++e) {
       mbar_init(bar(Br::kItemFull + e), 1);
-      mbar_init(bar(Br::kItemEmpty + e), 1 + 2 * BMH / 32);
+      mbar_init(bar(Br::kItemEmpty + e), 2 + 2 * BMH / 32);
     }
     *abort_flag = 0;
     fence_barrier_init();
@@ -222,6 +223,13 @@ causal_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
   };
   const int g = p.group_size;
   auto halves = [&](const WorkItem& it) { return it.n_nodes * g - it.row0 > BMH ? 2 : 1; };
+  // Key tiles of an item that half h takes part in: half A's rows may see nothing of the last one of an item with both halves
+  // (its 128 rows are at most 128 tokens, so all others concern both).
+  auto half_tiles = [&](const WorkItem& it, int h) {
+    const int T = it.tile_end - it.tile_begin;
+    const int last_key = it.prefix_len + ((it.row0 + BMH - 1) >> p.log2_g);          // of half A
+    return T - (h == 0 && T > 1 && halves(it) == 2 && last_key < (it.tile_end - 1) * BN ? 1 : 0);
+  };
 
   trigger_dependents();     // the next kernel of the stream may be scheduled; it waits for this grid before it touches what this one writes
   if (warp < 4) {
@@ -264,100 +272,131 @@ causal_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         }
       }
     }
-  } else if (warp == 1) {
-    // ------------------------------------------------------------------ tcgen05.mma issuer (one lane issues)
+  } else if (warp == 1 || warp == 3) {
+    // ------------------------------------------------------------------ tcgen05.mma issuers of half A / B (one lane issues)
+    // Batch by batch in turn: A's P V and next S, B's P V and next S, ...  What an issuer does between two batches -- waits
+    // for P, looks at the K and V barriers, commits -- runs under the other's batch; the turn passes through a named barrier.
+    // (One issuer for both: the pipe stood still 1 100 of 3 300 cycles a tile.  Two without turns: products interleave, both
+    // halves' S arrive together, both softmaxes run at once, and then the pipe waits: 4 430 cycles.)
+    const int h = warp == 1 ? 0 : 1;
     const bool elected = lane == 0;
-    TraceCursor trace = trace_open(p, 0, 3);
+    TraceCursor trace = trace_open(p, h == 0 ? 0 : 3, 4);
     if (!elected) trace.at = nullptr;
     constexpr uint32_t idesc_qk = make_idesc(BN, 0);
     constexpr uint32_t idesc_pv = make_idesc(D, 1);
     constexpr uint32_t kHi = desc_hi(1024);               // 8-row (8-key) groups 1024 bytes apart
-    const uint32_t q_lo0 = desc_lo(s_q, 16);
+    const uint32_t q_lo = desc_lo(s_q, 16) + uint32_t(h) * (L::kTileBytes >> 4);
     const uint32_t ring_k_lo0 = desc_lo(s_ring, 16);
     const uint32_t ring_v_lo0 = desc_lo(s_ring, L::kPanelBytes);   // MN-major: leading offset = next 64-column panel
-    auto issue_qk = [=](int h, uint32_t slot) {
-      const uint32_t a_lo = q_lo0 + uint32_t(h) * (L::kTileBytes >> 4);
+    const uint32_t t_s = tmem_base + uint32_t(h) * 128u, t_o = tmem_base + 256u + uint32_t(h) * 128u;
+    auto issue_qk = [=](uint32_t slot) {
       const uint32_t b_lo = ring_k_lo0 + __shfl_sync(0xffffffffu, slot, 0) * (L::kTileBytes >> 4);
       if (elect_one()) {
 #pragma unroll
         for (int ks = 0; ks < D / 16; ++ks) {
           const uint32_t off = (uint32_t(ks >> 2) * L::kPanelBytes + uint32_t(ks & 3) * 32u) >> 4;
-          umma_ss_lohi(tmem_base + uint32_t(h) * 128u, a_lo + off, kHi, b_lo + off, kHi, idesc_qk, ks > 0 ? 1u : 0u);
+          umma_ss_lohi(t_s, q_lo + off, kHi, b_lo + off, kHi, idesc_qk, ks > 0 ? 1u : 0u);
         }
       }
       __syncwarp();
     };
-    auto issue_pv = [=](int h, uint32_t slot, auto piece_tag, bool accumulate) {
+    auto issue_pv = [=](uint32_t slot, auto piece_tag, bool accumulate) {
       constexpr int kFrom = decltype(piece_tag)::value ? 2 * kFirstChunks : 0, kTo = decltype(piece_tag)::value ? BN / 16 : 2 * kFirstChunks;
       const uint32_t b_lo = ring_v_lo0 + __shfl_sync(0xffffffffu, slot, 0) * (L::kTileBytes >> 4);
       if (elect_one()) {
 #pragma unroll
         for (int kk = kFrom; kk < kTo; ++kk) {
-          umma_ts_lohi(tmem_base + 256u + uint32_t(h) * 128u, tmem_base + uint32_t(h) * 128u + uint32_t(kk) * 8u,
-                       b_lo + uint32_t(kk) * (2048u >> 4), kHi, idesc_pv, (accumulate || kk > kFrom) ? 1u : 0u);
+          umma_ts_lohi(t_o, t_s + uint32_t(kk) * 8u, b_lo + uint32_t(kk) * (2048u >> 4), kHi, idesc_pv,
+                       (accumulate || kk > kFrom) ? 1u : 0u);
         }
       }
       __syncwarp();
     };
-    auto commit = [&](int b) { if (elect_one()) tc_commit(bar(b)); };
-    constexpr uint32_t kNone = 0xffffffffu;
     uint32_t slot = 0, ph = 0;                            // ring position
-    uint32_t n_two = 0;                                   // items with both halves
+    uint32_t n_it = 0;                                    // items this half took part in
+    bool owed = false;                                    // half A: half B's last batch has not been waited for
     for (int w = 0; next_item(w); ++w) {
       const WorkItem item = item_of(w);
-      const int nh = halves(item);
-      const int T = item.tile_end - item.tile_begin;
-      mbar_wait(bar(Br::kSlotFull + slot), ph, abort_flag, p.status);
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        if (h >= nh) break;
-        mbar_wait(bar(Br::kQFull + h), (h == 0 ? uint32_t(w) : n_two) & 1u, abort_flag, p.status);
-        __syncwarp();
-        tc_fence_after();
-        issue_qk(h, slot);
-        commit(Br::kSReady + h);
+      const bool two = __shfl_sync(0xffffffffu, halves(item), 0) == 2;
+      const int T = __shfl_sync(0xffffffffu, item.tile_end - item.tile_begin, 0);
+      const int T_h = __shfl_sync(0xffffffffu, half_tiles(item, h), 0);
+      if (h == 1 && !two) {                               // no rows for this half: step over the item's tiles
+        slot += 2u * uint32_t(T);
+        ph ^= (slot / kSlots) & 1u;
+        slot %= kSlots;
+        continue;
       }
-      commit(Br::kSlotEmpty + slot);
-      if (T == 1) commit(Br::kQFree);
+      auto take_turn = [&]() {
+        if (!two) return;
+        __syncwarp();
+        if (h == 1 || owed) named_sync(kBarTurn + h, 64);
+        owed = true;
+      };
+      auto pass_turn = [&]() {
+        __syncwarp();
+        if (two) named_arrive(kBarTurn + 1 - h, 64);
+      };
+      // one of the two commits that free a slot / the Q tile (half A gives both where it is alone)
+      auto release = [&](int b) {
+        if (elect_one()) {
+          tc_commit(bar(b));
+          if (!two) tc_commit(bar(b));
+        }
+      };
+      mbar_wait(bar(Br::kQFull + h), (h == 0 ? uint32_t(w) : n_it) & 1u, abort_flag, p.status);
+      mbar_wait(bar(Br::kSlotFull + slot), ph, abort_flag, p.status);
+      take_turn();
+      tc_fence_after();
+      issue_qk(slot);
+      if (elect_one()) tc_commit(bar(Br::kSReady + h));
+      pass_turn();
+      release(Br::kSlotEmpty + slot);
+      if (T == 1) release(Br::kQFree);
       if (++slot == kSlots) { slot = 0; ph ^= 1u; }
-      // What runs between two batches of products is time that the pipe stands still: barriers are looked at where the issuer
-      // would wait for the second half of P anyway, the next K tile's in half A's turn, the next V tile's in the last one's.
-      bool v_here = false;
-      uint32_t freed = kNone;                             // the K slot that the last S products read, released behind the next batch
-      for (int j = 0; j < T; ++j) {
-        const bool more = j + 1 < T;
+      // A tile: O += P V in two pieces, behind it the next S (all tiles but the half's last)
+      auto tile = [&](int j, auto more_tag) {
+        constexpr bool kMore = decltype(more_tag)::value;
         const uint32_t vslot = slot, vph = ph;
         if (++slot == kSlots) { slot = 0; ph ^= 1u; }
         const uint32_t kslot = slot, kph = ph;
-        if (more && ++slot == kSlots) { slot = 0; ph ^= 1u; }
-        if (!v_here) mbar_wait(bar(Br::kSlotFull + vslot), vph, abort_flag, p.status);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          if (h >= nh) break;
-          if (j == 0) mbar_wait(bar(Br::kOFree + h), ((h == 0 ? uint32_t(w) : n_two) & 1u) ^ 1u, abort_flag, p.status);
-          __syncwarp();
-          named_sync(kBarP + 2 * h, kPCount);
-          tc_fence_after();
-          trace_event(trace, DYSPEC_TAG(0, 1 + 4 * h, j));
-          issue_pv(h, vslot, std::integral_constant<int, 0>{}, j > 0);
-          if (h == 0 && freed != kNone) commit(Br::kSlotEmpty + freed);
-          if (h == 0 && more) mbar_wait(bar(Br::kSlotFull + kslot), kph, abort_flag, p.status);
-          if (h + 1 == nh && more) v_here = mbar_test_wait(bar(Br::kSlotFull + slot), ph);
-          __syncwarp();
-          named_sync(kBarP + 2 * h + 1, kPCount);
-          tc_fence_after();
-          trace_event(trace, DYSPEC_TAG(0, 3 + 4 * h, j));
-          issue_pv(h, vslot, std::integral_constant<int, 1>{}, true);
-          trace_event(trace, DYSPEC_TAG(0, 2 + 4 * h, j));
-          if (h + 1 == nh) commit(Br::kSlotEmpty + vslot);
-          if (more) issue_qk(h, kslot);
-          commit(more ? Br::kSReady + h : Br::kODone + h);
-          trace_event(trace, DYSPEC_TAG(0, 4 + 4 * h, j));
-        }
-        freed = more ? kslot : kNone;
-        if (j + 2 == T) { commit(Br::kQFree); commit(Br::kSlotEmpty + kslot); freed = kNone; }
+        if (kMore && ++slot == kSlots) { slot = 0; ph ^= 1u; }
+        const uint32_t got = kMore ? mbar_test_wait2(bar(Br::kSlotFull + vslot), vph, bar(Br::kSlotFull + kslot), kph) : 2u;
+        if (!(got & 1u)) mbar_wait(bar(Br::kSlotFull + vslot), vph, abort_flag, p.status);
+        if (!(got & 2u)) mbar_wait(bar(Br::kSlotFull + kslot), kph, abort_flag, p.status);
+        if (j == 0) mbar_wait(bar(Br::kOFree + h), (n_it & 1u) ^ 1u, abort_flag, p.status);
+        __syncwarp();
+        named_sync(kBarP + 2 * h, kPCount);
+        trace_event(trace, DYSPEC_TAG(3 * h, 1, j));
+        take_turn();
+        tc_fence_after();
+        trace_event(trace, DYSPEC_TAG(3 * h, 2, j));
+        issue_pv(vslot, std::integral_constant<int, 0>{}, j > 0);
+        __syncwarp();
+        named_sync(kBarP + 2 * h + 1, kPCount);
+        tc_fence_after();
+        trace_event(trace, DYSPEC_TAG(3 * h, 3, j));
+        issue_pv(vslot, std::integral_constant<int, 1>{}, true);
+        if constexpr (kMore) issue_qk(kslot);
+        if (elect_one()) tc_commit(bar((kMore ? Br::kSReady : Br::kODone) + h));
+        trace_event(trace, DYSPEC_TAG(3 * h, 4, j));
+        pass_turn();
+        release(Br::kSlotEmpty + vslot);
+        if constexpr (kMore) release(Br::kSlotEmpty + kslot);
+      };
+#pragma unroll 1
+      for (int j = 0; j + 1 < T_h; ++j) tile(j, std::true_type{});
+      if (T_h == T && T > 1) release(Br::kQFree);         // (the last S product of this half has been issued)
+      tile(T_h - 1, std::false_type{});
+      if (T_h < T) {                                      // half A steps over the item's last K and V tile
+        release(Br::kSlotEmpty + slot);
+        if (++slot == kSlots) { slot = 0; ph ^= 1u; }
+        release(Br::kQFree);
+        take_turn();
+        pass_turn();
+        release(Br::kSlotEmpty + slot);
+        if (++slot == kSlots) { slot = 0; ph ^= 1u; }
       }
-      n_two += nh == 2 ? 1u : 0u;
+      ++n_it;
     }
   }
   } else {
@@ -372,20 +411,17 @@ causal_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     const uint32_t t_s = tmem_base + uint32_t(h) * 128u + lane_sel;             // scores, then probabilities (bf16 pairs)
     const uint32_t t_o = tmem_base + 256u + uint32_t(h) * 128u + lane_sel;
     uint32_t n_s = 0, n_o = 0;                           // S-ready / O-done phases seen
-    uint32_t slot = 0, ph = 0;                           // ring position of the next K tile (its V tile follows)
+    uint32_t ring = 0;                                   // K and V tiles of earlier items
     TraceCursor trace = trace_open(p, 1 + h, 3);
     if (r != 0) trace.at = nullptr;
 
     for (int w = 0; next_item(w); ++w) {
       const WorkItem item = item_of(w);
       const int n_rows = item.n_nodes * g;
-      const int T = item.tile_end - item.tile_begin;
-      if (h >= halves(item)) {
-        slot += 2u * uint32_t(T);
-        ph ^= (slot / kSlots) & 1u;
-        slot %= kSlots;
-        continue;
-      }
+      const uint32_t ring0 = ring;                                  // K tile j at ring position ring0 + 2 j, its V tile behind it
+      ring += 2u * uint32_t(item.tile_end - item.tile_begin);
+      if (h >= halves(item)) continue;
+      const int T = half_tiles(item, h);
       const int row = item.row0 + h * BMH + r;
       const bool ok = row < n_rows;
       const int token = min(row >> p.log2_g, item.n_nodes - 1);     // (rows behind the last one follow it; they are not written)
@@ -397,10 +433,6 @@ causal_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         const int vis = last_key + 1 - key0;                        // how many of the tile's keys the row sees (<= 0: none, >= 128: all)
         const bool all_visible = __all_sync(0xffffffffu, vis >= BN);
         const int own = item.prefix_len + item.n_nodes - key0;      // how many of them belong to the sequence
-        if (++slot == kSlots) { slot = 0; ph ^= 1u; }               // (slot, ph: now the V tile's)
-        const uint32_t vslot = slot, vph = ph;
-        if (++slot == kSlots) { slot = 0; ph ^= 1u; }
-
         mbar_wait(bar(Br::kSReady + h), n_s & 1u, abort_flag, p.status);
         ++n_s;
         __syncwarp();
@@ -505,13 +537,16 @@ causal_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             m_used = m_new;
           }
           // V rows behind the end of the sequence are not ours: zero them (their probabilities are 0, but 0 * garbage could be
-          // NaN).  Both halves do, each before it publishes its P: neither's product waits for the other half.
+          // NaN), a row per thread, chunks in an order that spreads the banks.  Both halves do, each before it publishes its P:
+          // neither's product waits for the other half.
           if (own < BN) {
-            mbar_wait(bar(Br::kSlotFull + vslot), vph, abort_flag, p.status);
-            uint8_t* v_tile = smem + L::kRingOffset + vslot * L::kTileBytes;
-            for (int idx = r; idx < (BN - own) * 8 * L::kPanels; idx += BMH) {
-              const int pn = idx / ((BN - own) * 8), rem = idx % ((BN - own) * 8);
-              *reinterpret_cast<uint4*>(v_tile + pn * L::kPanelBytes + (own + rem / 8) * 128 + (rem % 8) * 16) = make_uint4(0u, 0u, 0u, 0u);
+            const uint32_t at = ring0 + 2u * uint32_t(j) + 1u, vslot = at % kSlots;
+            mbar_wait(bar(Br::kSlotFull + vslot), (at / kSlots) & 1u, abort_flag, p.status);
+            if (r >= own) {
+              uint8_t* v_row = smem + L::kRingOffset + vslot * L::kTileBytes + r * 128;
+#pragma unroll
+              for (int i = 0; i < 8 * L::kPanels; ++i)
+                *reinterpret_cast<uint4*>(v_row + (i >> 3) * L::kPanelBytes + ((r + i) & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
             }
             fence_proxy_async();
             __syncwarp();
@@ -535,6 +570,7 @@ causal_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
       ++n_o;
       __syncwarp();
       tc_fence_after();
+      trace_event(trace, DYSPEC_TAG(1 + h, 6, 0));
       if (!dep_ok) {
         grid_dependency_wait();                            // global writes from here on
         dep_ok = true;
@@ -576,6 +612,7 @@ causal_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
           slot_at[2 * BMH * D + 2 * BMH + pr] = l;
         }
       }
+      trace_event(trace, DYSPEC_TAG(1 + h, 7, 0));
     }
   }
 
