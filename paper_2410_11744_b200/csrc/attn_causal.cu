@@ -5,17 +5,31 @@
 // One CTA per SM, 12 warps; a work item is 256 packed query rows of one (request, kv head), two halves A and B of 128, against
 // a range of 128-key tiles:
 //   warp 0       TMA producer: the item's Q (half A, then B), then K and V tiles into a shared-memory ring;
-//   warp 1       issues tcgen05.mma: S = Q K^T (both operands in shared memory), O += P V (P in tensor memory);
+//   warps 1, 3   issue tcgen05.mma for half A / B: S = Q K^T (both operands in shared memory), O += P V (P in tensor memory);
 //   warp 2       tensor memory: S_A, S_B (128 fp32 columns each), O_A, O_B (D each);
 //   warps 4-7    softmax of half A, a row per thread: fp32 online softmax in the exp2 domain; warps 8-11 of half B.
 // A half's P (bf16) takes the place of its S: a thread has its row of scores in registers before it writes the first
 // probability.  Products of one issuing thread run in order, so S(j + 1), issued behind P V(j), overwrites a P that has
 // been read, and "S(j + 1) is there" also says that P V(j) is done: one barrier tells the softmax threads both, and the
-// running output may be rescaled then without another wait.  One thread issues for both halves: P V and the next S of A, then
-// those of B, and so on, and the softmax of one half runs under the products of the other.  (An issuer per half, as in the tree
-// kernel, has its products interleaved with the other's: both halves' S arrive together, both softmaxes run at once and the
-// pipe waits for them, 4 430 cycles a tile.)
-// P is handed over in two pieces of 64 keys, so that the first half of P V runs under the second half of the exponentials.
+// running output may be rescaled then without another wait.
+//
+// What bounds it.  A tile is 2 048 cycles of the tensor pipe (D = 128, both halves), 2 048 of the exponential unit if it did all
+// exponentials, and about 1 200 issue slots of each scheduler; the chain of one half, S -> row -> weights -> P V -> next S, is
+// 3 000, of which the other half's products hide what they can.  Measured 3 150 - 3 300 cycles a tile: 512 tokens over 8192 keys
+// (64 / 8 heads of 128) 105 - 108 us warm, 1.3 PFLOP/s; a prompt of 16384 3.3 - 3.8 ms, 1.15 - 1.35 PFLOP/s, under the power cap.  What
+// it took, each measured against the step before on those 512 tokens:
+//   - Issuing in turns, A's P V and next S, then B's (153 -> 143 us).  Without turns both halves' products interleave, their S
+//     arrive together, both softmaxes run at once, and then the pipe waits for them: 4 430 cycles.
+//   - tcgen05.mma operands that the compiler knows to be uniform (elect.sync, values through a shuffle): 143 -> 122.  From ordinary
+//     registers each product took 90 - 120 cycles to issue instead of 64.
+//   - Weights against the old reference beside the maximum, not behind it; P handed over in two pieces of 64 keys, so that
+//     the first half of P V runs under the second half of the weights (pieces of 32 + 96 or 96 + 32: 5 % slower).
+//   - An issuer per half, so that one's waits and commits run under the other's batch (2 - 3 %).
+//   - 6 of 16 pairs of exponentials on the FMA pipe (4: 2 % slower; 0: 5 - 8 %; 8: 3 %).
+// Tried and slower: two threads per row (16 softmax warps, 104 registers: 130 - 138); one S buffer that the halves share, with P
+// beside it, as in the tree kernel (123); for D = 64, whose tensor memory has the room, P beside two S buffers (193 -> 221:
+// both softmaxes at once again); one issuer that asks for the next item's S before this one's output is out (long prompts + 3 %).
+// Neither half the loads (timing only) nor a finer ring changed anything.
 //
 // CTAs take items from a queue, longest first (see schedule_causal in api.cu); an item whose group was cut along the
 // keys writes an fp32 partial (O, m, l) that combine_kernel merges.  Every wait on an mbarrier is bounded (see mbar_wait).
@@ -50,7 +64,7 @@ struct Bars {
   static constexpr int kQFull = 0;                      // [2] query half A / B is in shared memory
   static constexpr int kQFree = 2;                      // the item's last S products have run
   static constexpr int kSlotFull = 3;                   // [kSlots]
-  static constexpr int kSlotEmpty = kSlotFull + kSlots; // [kSlots]
+  static constexpr int kSlotEmpty = kSlotFull + kSlots; // [kSlots] two commits, one per issuer
   static constexpr int kSReady = kSlotEmpty + kSlots;   // [2]
   static constexpr int kODone = kSReady + 2;            // [2] the item's last P V has run
   static constexpr int kOFree = kODone + 2;             // [2] the output has been read out
@@ -79,14 +93,7 @@ __device__ __forceinline__ uint64_t exp2_poly2(uint64_t x2) {
   return pack_f32x2(__uint_as_float(__float_as_uint(p0) + (__float_as_uint(t0) << 23)),
                     __uint_as_float(__float_as_uint(p1) + (__float_as_uint(t1) << 23)));
 }
-#ifndef REG_LO
-#define REG_LO "64"
-#define REG_HI "216"
-#endif
-#ifndef POLY
-#define POLY 4
-#endif
-constexpr int kPolyPairs = POLY;             // of the 16 pairs in 32 keys, how many take the polynomial
+constexpr int kPolyPairs = 6;             // of the 16 pairs in 32 keys, how many take the polynomial
 __device__ __forceinline__ float max3_nan(float a, float b, float c) {
   float d;
   asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
@@ -98,9 +105,9 @@ __device__ __forceinline__ float max_nan(float a, float b) {
   return d;
 }
 
-// Trace tags (see dyspec_set_trace): role << 14 | event << 10 | key-tile index; role 0 = issuer, 1 / 2 = softmax row 0 of half A / B.
-// Issuer events (half B: + 4): 1 / 3 first / second 64 keys of P seen, 2 P V issued, 4 next S issued.  Softmax events: 1 S seen, 2
-// row loaded, 3 maximum known, 4 / 5 first / second 64 keys of P published.
+// Trace tags (see dyspec_set_trace): role << 14 | event << 10 | key-tile index; roles 0 / 3 = issuer of half A / B, 1 / 2 = softmax row 0
+// of half A / B.  Issuer events: 1 / 3 first / second 64 keys of P seen, 2 turn taken, 4 products issued.  Softmax events: 1 S seen, 2
+// row loaded, 3 maximum known, 4 / 5 first / second 64 keys of P published, 6 last P V seen, 7 output written.
 #define DYSPEC_TAG(role, event, j) ((uint32_t(role) << 14) | (uint32_t(event) << 10) | (uint32_t(j) & 1023u))
 
 // One lane of the warp, and the compiler knows that it is one: what feeds a tcgen05 instruction stays in uniform registers.
@@ -110,10 +117,7 @@ __device__ __forceinline__ bool elect_one() {
   return one != 0;
 }
 
-#ifndef SPLIT
-#define SPLIT 2
-#endif
-constexpr int kFirstChunks = SPLIT;          // P is handed over in two pieces: 32 * kFirstChunks keys, then the rest
+constexpr int kFirstChunks = 2;          // P is handed over in two pieces: 32 * kFirstChunks keys, then the rest
 constexpr int kBarP = 1;                    // named barriers 1 .. 4: 64 keys of P are in tensor memory (half A: 1, 2; half B: 3, 4)
 constexpr int kBarTurn = 5;                 // named barriers 5, 6: half A's / half B's turn to issue
 constexpr int kPCount = BMH + 32;           // a half's softmax threads + the issuing warp
@@ -233,7 +237,7 @@ causal_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 
   trigger_dependents();     // the next kernel of the stream may be scheduled; it waits for this grid before it touches what this one writes
   if (warp < 4) {
-  asm volatile("setmaxnreg.dec.sync.aligned.u32 " REG_LO ";");
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
   if (warp == 0) {
     // ------------------------------------------------------------------ TMA producer (one lane issues)
     const bool elected = lane == 0;
@@ -274,10 +278,7 @@ causal_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     }
   } else if (warp == 1 || warp == 3) {
     // ------------------------------------------------------------------ tcgen05.mma issuers of half A / B (one lane issues)
-    // Batch by batch in turn: A's P V and next S, B's P V and next S, ...  What an issuer does between two batches -- waits
-    // for P, looks at the K and V barriers, commits -- runs under the other's batch; the turn passes through a named barrier.
-    // (One issuer for both: the pipe stood still 1 100 of 3 300 cycles a tile.  Two without turns: products interleave, both
-    // halves' S arrive together, both softmaxes run at once, and then the pipe waits: 4 430 cycles.)
+    // Batch by batch in turn: A's P V and next S, B's P V and next S, ...; the turn passes through a named barrier.
     const int h = warp == 1 ? 0 : 1;
     const bool elected = lane == 0;
     TraceCursor trace = trace_open(p, h == 0 ? 0 : 3, 4);
@@ -400,7 +401,7 @@ causal_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     }
   }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 " REG_HI ";");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
     // ------------------------------------------------------------------ softmax + epilogue warps
     // Q, K, V and the work items are inputs that no kernel launched with early start writes; only the output and the
     // partials wait for the preceding kernels of the stream.
@@ -412,7 +413,7 @@ causal_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     const uint32_t t_o = tmem_base + 256u + uint32_t(h) * 128u + lane_sel;
     uint32_t n_s = 0, n_o = 0;                           // S-ready / O-done phases seen
     uint32_t ring = 0;                                   // K and V tiles of earlier items
-    TraceCursor trace = trace_open(p, 1 + h, 3);
+    TraceCursor trace = trace_open(p, 1 + h, 4);
     if (r != 0) trace.at = nullptr;
 
     for (int w = 0; next_item(w); ++w) {
