@@ -32,7 +32,7 @@
 // Neither half the loads (timing only) nor a finer ring changed anything.
 //
 // CTAs take items from a queue, longest first (see schedule_causal in api.cu); an item whose group was cut along the
-// keys writes an fp32 partial (O, m, l) that combine_kernel merges.  Every wait on an mbarrier is bounded (see mbar_wait).
+// keys writes an fp32 partial (O, m, l) that combine_kernel merges.  Every wait on an mbarrier is bounded (see mbar_wait_idle).
 #include "tc_ops.cuh"
 #include <type_traits>
 
@@ -117,6 +117,22 @@ __device__ __forceinline__ bool elect_one() {
   return one != 0;
 }
 
+
+// Bounded wait on an mbarrier as mbar_wait, but suspended by the hardware from the start instead of polling at first: what a
+// waiting warp issues here is taken from the softmax warps of its scheduler (polling: 3 - 7 % slower).
+__device__ __forceinline__ bool mbar_wait_idle(uint32_t bar, uint32_t parity, volatile int* abort_flag, int32_t* status) {
+  if (mbar_try_wait(bar, parity)) return true;
+  const uint64_t t0 = global_timer_ns();
+  while (!mbar_try_wait(bar, parity)) {
+    if (*abort_flag) return false;
+    if (global_timer_ns() - t0 > kWaitLimitNs) {
+      *abort_flag = 1;
+      if (status) atomicCAS(status, 0, DYSPEC_ERR_TIMEOUT);
+      return false;
+    }
+  }
+  return true;
+}
 constexpr int kFirstChunks = 2;          // P is handed over in two pieces: 32 * kFirstChunks keys, then the rest
 constexpr int kBarP = 1;                    // named barriers 1 .. 4: 64 keys of P are in tensor memory (half A: 1, 2; half B: 3, 4)
 constexpr int kBarTurn = 5;                 // named barriers 5, 6: half A's / half B's turn to issue
@@ -195,7 +211,7 @@ causal_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     if (lane == 0) {
       if (w == 1) grid_dependency_wait();                  // the last launch on this workspace cleared the queue words
       const int t = atomicAdd(p.queue, 1) + int(gridDim.x);
-      if (w > 8) mbar_wait(bar(Br::kItemEmpty + ((w - 1) & 7)), (uint32_t((w - 1) >> 3) & 1u) ^ 1u, abort_flag, p.status);
+      if (w > 8) mbar_wait_idle(bar(Br::kItemEmpty + ((w - 1) & 7)), (uint32_t((w - 1) >> 3) & 1u) ^ 1u, abort_flag, p.status);
       idx = t < p.n_items_total ? t : -1;
       ring_idx[(w - 1) & 7] = idx;
       if (idx >= 0) {
@@ -218,7 +234,7 @@ causal_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     // The producer publishes every item in bounded time, whatever other waits ran out: a role that is in its error state still
     // goes through the items that the others go through, so that all of them meet at the named barriers.
     const uint32_t at = bar(Br::kItemFull + ((w - 1) & 7)), parity = uint32_t((w - 1) >> 3) & 1u;
-    if (!mbar_wait(at, parity, abort_flag, p.status)) {
+    if (!mbar_wait_idle(at, parity, abort_flag, p.status)) {
       const uint64_t t0 = global_timer_ns();
       while (!mbar_test_wait(at, parity))
         if (global_timer_ns() - t0 > 8 * kWaitLimitNs) return false;
@@ -250,7 +266,7 @@ causal_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     for (int w = 0; take_item(w); ++w) {
       const WorkItem item = item_of(w, false);
       const int nh = halves(item);
-      mbar_wait(bar(Br::kQFree), (uint32_t(w) & 1u) ^ 1u, abort_flag, p.status);
+      mbar_wait_idle(bar(Br::kQFree), (uint32_t(w) & 1u) ^ 1u, abort_flag, p.status);
       // half A, the first K tile, half B: the item's first product needs only the first two
       auto load_q_half = [&](int h) {
         if (elected) {
@@ -264,7 +280,7 @@ causal_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
       for (int t = item.tile_begin; t < item.tile_end; ++t) {
         const int64_t row = causal_tile_row(p, item, t, BN);
         for (int kv = 0; kv < 2; ++kv) {
-          mbar_wait(bar(Br::kSlotEmpty + slot), ph ^ 1u, abort_flag, p.status);
+          mbar_wait_idle(bar(Br::kSlotEmpty + slot), ph ^ 1u, abort_flag, p.status);
           if (elected) {
             mbar_expect_tx(bar(Br::kSlotFull + slot), L::kTileBytes);
             for (int pn = 0; pn < L::kPanels; ++pn)
@@ -344,8 +360,8 @@ causal_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
           if (!two) tc_commit(bar(b));
         }
       };
-      mbar_wait(bar(Br::kQFull + h), (h == 0 ? uint32_t(w) : n_it) & 1u, abort_flag, p.status);
-      mbar_wait(bar(Br::kSlotFull + slot), ph, abort_flag, p.status);
+      mbar_wait_idle(bar(Br::kQFull + h), (h == 0 ? uint32_t(w) : n_it) & 1u, abort_flag, p.status);
+      mbar_wait_idle(bar(Br::kSlotFull + slot), ph, abort_flag, p.status);
       take_turn();
       tc_fence_after();
       issue_qk(slot);
@@ -362,9 +378,9 @@ causal_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         const uint32_t kslot = slot, kph = ph;
         if (kMore && ++slot == kSlots) { slot = 0; ph ^= 1u; }
         const uint32_t got = kMore ? mbar_test_wait2(bar(Br::kSlotFull + vslot), vph, bar(Br::kSlotFull + kslot), kph) : 2u;
-        if (!(got & 1u)) mbar_wait(bar(Br::kSlotFull + vslot), vph, abort_flag, p.status);
-        if (!(got & 2u)) mbar_wait(bar(Br::kSlotFull + kslot), kph, abort_flag, p.status);
-        if (j == 0) mbar_wait(bar(Br::kOFree + h), (n_it & 1u) ^ 1u, abort_flag, p.status);
+        if (!(got & 1u)) mbar_wait_idle(bar(Br::kSlotFull + vslot), vph, abort_flag, p.status);
+        if (!(got & 2u)) mbar_wait_idle(bar(Br::kSlotFull + kslot), kph, abort_flag, p.status);
+        if (j == 0) mbar_wait_idle(bar(Br::kOFree + h), (n_it & 1u) ^ 1u, abort_flag, p.status);
         __syncwarp();
         named_sync(kBarP + 2 * h, kPCount);
         trace_event(trace, DYSPEC_TAG(3 * h, 1, j));
@@ -434,7 +450,7 @@ causal_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         const int vis = last_key + 1 - key0;                        // how many of the tile's keys the row sees (<= 0: none, >= 128: all)
         const bool all_visible = __all_sync(0xffffffffu, vis >= BN);
         const int own = item.prefix_len + item.n_nodes - key0;      // how many of them belong to the sequence
-        mbar_wait(bar(Br::kSReady + h), n_s & 1u, abort_flag, p.status);
+        mbar_wait_idle(bar(Br::kSReady + h), n_s & 1u, abort_flag, p.status);
         ++n_s;
         __syncwarp();
         tc_fence_after();
@@ -542,7 +558,7 @@ causal_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
           // neither's product waits for the other half.
           if (own < BN) {
             const uint32_t at = ring0 + 2u * uint32_t(j) + 1u, vslot = at % kSlots;
-            mbar_wait(bar(Br::kSlotFull + vslot), (at / kSlots) & 1u, abort_flag, p.status);
+            mbar_wait_idle(bar(Br::kSlotFull + vslot), (at / kSlots) & 1u, abort_flag, p.status);
             if (r >= own) {
               uint8_t* v_row = smem + L::kRingOffset + vslot * L::kTileBytes + r * 128;
 #pragma unroll
@@ -567,7 +583,7 @@ causal_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
       }
 
       // ---- epilogue: wait for the last P V, read O, normalise (or emit the partial)
-      mbar_wait(bar(Br::kODone + h), n_o & 1u, abort_flag, p.status);
+      mbar_wait_idle(bar(Br::kODone + h), n_o & 1u, abort_flag, p.status);
       ++n_o;
       __syncwarp();
       tc_fence_after();
