@@ -118,21 +118,6 @@ __device__ __forceinline__ bool elect_one() {
 }
 
 
-// Bounded wait on an mbarrier as mbar_wait, but suspended by the hardware from the start instead of polling at first: what a
-// waiting warp issues here is taken from the softmax warps of its scheduler (polling: 3 - 7 % slower).
-__device__ __forceinline__ bool mbar_wait_idle(uint32_t bar, uint32_t parity, volatile int* abort_flag, int32_t* status) {
-  if (mbar_try_wait(bar, parity)) return true;
-  const uint64_t t0 = global_timer_ns();
-  while (!mbar_try_wait(bar, parity)) {
-    if (*abort_flag) return false;
-    if (global_timer_ns() - t0 > kWaitLimitNs) {
-      *abort_flag = 1;
-      if (status) atomicCAS(status, 0, DYSPEC_ERR_TIMEOUT);
-      return false;
-    }
-  }
-  return true;
-}
 constexpr int kFirstChunks = 2;          // P is handed over in two pieces: 32 * kFirstChunks keys, then the rest
 constexpr int kBarP = 1;                    // named barriers 1 .. 4: 64 keys of P are in tensor memory (half A: 1, 2; half B: 3, 4)
 constexpr int kBarTurn = 5;                 // named barriers 5, 6: half A's / half B's turn to issue

@@ -144,6 +144,12 @@ __device__ __forceinline__ void tmem_st_rows(uint32_t taddr, const float (&v)[NJ
       : "memory");
 }
 
+template <bool kIdle>
+__device__ __forceinline__ bool wait_bar(uint32_t bar, uint32_t parity, volatile int* abort_flag, int32_t* status) {
+  if constexpr (kIdle) return mbar_wait_idle(bar, parity, abort_flag, status);
+  else return mbar_wait(bar, parity, abort_flag, status);
+}
+
 // One row of a split group, by one warp: out = (sum_s w_s O_s) / (sum_s w_s l_s), w_s = 2^(m_s - max m).  Every lane holds
 // the pieces' maxima and sums 32 pieces at a time, and D / 32 columns; four pieces' columns are in flight.
 template <int D>
@@ -303,7 +309,7 @@ tree_attn_small_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
         const WorkItem item = item_of(w);
         const WorkItem& rq = item;
         // Q tile: box (64 cols, g heads, BM/g nodes) per panel; rows land node-major, head-minor.
-        mbar_wait(bar_qempty, (qit & 1) ^ 1, abort_flag, p.status);
+        wait_bar<kCausal>(bar_qempty, (qit & 1) ^ 1, abort_flag, p.status);
         mbar_expect_tx(bar_qfull, L::kQBytes);
         for (int h = 0; h < L::kHalves; ++h)
           tma_load_3d(s_q + h * (BM * 128), &map_q, bar_qfull, h * 64, item.kv_head * g,
@@ -313,7 +319,7 @@ tree_attn_small_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
           const int stage = ring_stage;
           const uint32_t ph = ring_phase;
           if (++ring_stage == n_stages) { ring_stage = 0; ring_phase ^= 1u; }
-          mbar_wait(bar_empty + 8 * stage, ph ^ 1, abort_flag, p.status);
+          wait_bar<kCausal>(bar_empty + 8 * stage, ph ^ 1, abort_flag, p.status);
           const int64_t row = kCausal ? causal_tile_row(p, item, t, BN) : kv_tile_row(p, item, t, n_prefix_tiles, BN);
           const uint32_t dst = s_kv + stage * L::kStageBytes;
           mbar_expect_tx(bar_full + 8 * stage, L::kStageBytes);
@@ -339,15 +345,15 @@ tree_attn_small_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
       for (int w = item_begin; w < item_end; ++w, ++qit) {
         const WorkItem item = item_of(w);
         const int T = item.tile_end - item.tile_begin;
-        mbar_wait(bar_qfull, qit & 1, abort_flag, p.status);
+        wait_bar<kCausal>(bar_qfull, qit & 1, abort_flag, p.status);
         for (int i = 0; i < T; ++i, ++pos) {
           const int sb = pos & (kSBufs - 1), sb_use = pos / kSBufs;
           // Which of the two comes last depends on the side that is slower, loads or softmax, and a probe costs some 180
           // cycles, so both go out together.  (A buffer's first use: the parity that a fresh barrier has behind it.)
           const uint32_t sf_ph = uint32_t(sb_use - 1) & 1u;
           const uint32_t got = mbar_test_wait2(bar_sfree + 8 * sb, sf_ph, bar_full + 8 * stage, ph);
-          if (!(got & 1u)) mbar_wait(bar_sfree + 8 * sb, sf_ph, abort_flag, p.status);
-          if (!(got & 2u)) mbar_wait(bar_full + 8 * stage, ph, abort_flag, p.status);
+          if (!(got & 1u)) wait_bar<kCausal>(bar_sfree + 8 * sb, sf_ph, abort_flag, p.status);
+          if (!(got & 2u)) wait_bar<kCausal>(bar_full + 8 * stage, ph, abort_flag, p.status);
           tc_fence_after();
           const uint32_t k_lo = desc_lo(s_kv + stage * L::kStageBytes);
 #pragma unroll
@@ -377,12 +383,12 @@ tree_attn_small_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
         const int T = item.tile_end - item.tile_begin;
         for (int m = 0; m < T; ++m) {
           const int pv_set = m & 1;
-          if (m < 2 && qit > 0) mbar_wait(bar_ofree, (qit - 1) & 1u, abort_flag, p.status);   // first product into this accumulator
+          if (m < 2 && qit > 0) wait_bar<kCausal>(bar_ofree, (qit - 1) & 1u, abort_flag, p.status);   // first product into this accumulator
           // V is under the TMA's own barrier, and this warp waits for it itself: that P is ready says no more than that
           // K has landed.  V came long before P, so the two probes go out together.
           const uint32_t got = mbar_test_wait2(bar_full + 8 * stage, ph, bar_pready + 8 * stage, ph);
-          if (!(got & 1u)) mbar_wait(bar_full + 8 * stage, ph, abort_flag, p.status);
-          if (!(got & 2u)) mbar_wait(bar_pready + 8 * stage, ph, abort_flag, p.status);
+          if (!(got & 1u)) wait_bar<kCausal>(bar_full + 8 * stage, ph, abort_flag, p.status);
+          if (!(got & 2u)) wait_bar<kCausal>(bar_pready + 8 * stage, ph, abort_flag, p.status);
           tc_fence_after();
           const uint32_t p_lo = desc_lo(s_kv + stage * L::kStageBytes);                        // P sits where the K tile was
           const uint32_t v_lo = desc_lo(s_kv + stage * L::kStageBytes + L::kTileBytes) - (1u << 16) + ((uint32_t(L::kPanelBytes) >> 4) << 16);
@@ -428,7 +434,7 @@ tree_attn_small_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
   // Afterwards every product of this set issued so far has landed.
   auto confirm_pv_done = [&](bool seen) {
     if (pv_seen < n_pv) {
-      if (!seen) mbar_wait(bar_pvdone + 8 * set, uint32_t(pv_seen) & 1u, abort_flag, p.status);
+      if (!seen) wait_bar<kCausal>(bar_pvdone + 8 * set, uint32_t(pv_seen) & 1u, abort_flag, p.status);
       ++pv_seen;
     }
     __syncwarp();            // (what follows, tensor-memory accesses and barriers, is the whole warp's)
@@ -492,7 +498,7 @@ tree_attn_small_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
       // (the probe of the set's previous product rides along: its answer is not needed before the maxima are known)
       const uint32_t sph = uint32_t(pos / kSBufs) & 1u;
       const uint32_t got = mbar_test_wait2(bar_sfull + 8 * sb, sph, bar_pvdone + 8 * set, uint32_t(pv_seen) & 1u);
-      if (!(got & 1u)) mbar_wait(bar_sfull + 8 * sb, sph, abort_flag, p.status);
+      if (!(got & 1u)) wait_bar<kCausal>(bar_sfull + 8 * sb, sph, abort_flag, p.status);
       __syncwarp();          // (the lanes' probes may differ, and the load below is one of the whole warp)
       tc_fence_after();
       if (threadIdx.x == 0 && w == item_begin && t == item.tile_begin) stamp(3);
@@ -640,7 +646,7 @@ tree_attn_small_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
       //      caller never wrote): zero them so that 0 * garbage cannot produce NaN (their probabilities
       //      are exactly 0).  Every compute warp writes the same zeros before its own reads.
       if (own < BN) {
-        mbar_wait(bar_full + 8 * stage, ph, abort_flag, p.status);   // (complete by now: it makes the TMA's writes of V visible to this thread)
+        wait_bar<kCausal>(bar_full + 8 * stage, ph, abort_flag, p.status);   // (complete by now: it makes the TMA's writes of V visible to this thread)
         for (int idx = lane; idx < (BN - own) * (D / 8); idx += 32) {
           const int row = own + idx / (D / 8), chunk = idx % (D / 8);
           asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(s_v + swz(row, chunk, L::kPanelBytes)), "r"(0u) : "memory");
@@ -797,7 +803,7 @@ tree_attn_small_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
           if (pool_a) { s_ = __ffs(pool_a) - 1; pool_a &= pool_a - 1u; }
           else { s_ = __ffs(pool_b) - 1; pool_b &= pool_b - 1u; }
           const bool last = k_src == C - 2;
-          mbar_wait(bar_src + 8 * s_, 0, abort_flag, p.status);
+          wait_bar<kCausal>(bar_src + 8 * s_, 0, abort_flag, p.status);
           const float* src_o = recv + (s_ < rank ? s_ : s_ - 1) * chunk_floats;
           const float* src_m = src_o + R * D;
           const float* src_l = src_m + R;
