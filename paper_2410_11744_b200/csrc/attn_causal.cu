@@ -390,13 +390,15 @@ causal_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
       if (T_h == T && T > 1) release(Br::kQFree);         // (the last S product of this half has been issued)
       tile(T_h - 1, std::false_type{});
       if (T_h < T) {                                      // half A steps over the item's last K and V tile
-        release(Br::kSlotEmpty + slot);
-        if (++slot == kSlots) { slot = 0; ph ^= 1u; }
         release(Br::kQFree);
         take_turn();
         pass_turn();
-        release(Br::kSlotEmpty + slot);
-        if (++slot == kSlots) { slot = 0; ph ^= 1u; }
+        for (int kv = 0; kv < 2; ++kv) {                  // (released once they are there: the slot's earlier use is over then)
+          mbar_wait_idle(bar(Br::kSlotFull + slot), ph, abort_flag, p.status);
+          __syncwarp();
+          release(Br::kSlotEmpty + slot);
+          if (++slot == kSlots) { slot = 0; ph ^= 1u; }
+        }
       }
       ++n_it;
     }
