@@ -513,10 +513,12 @@ causal_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         constexpr std::integral_constant<int, kPolyPairs> kMixed{};
         // The reference almost always stays: the first weights are computed against the one there is, beside the maximum
         // instead of behind it, and again in the rare tile that raises it.
-        bool careful = j == 0 || !all_visible || !__all_sync(0xffffffffu, fabsf(m_used) <= kCoarseReference);
+        // (Rows that are not the request's have no vote: what their Q holds changes no bit of the others.)
+        const bool raised = ok && !(m_new <= m_used + kRescaleThreshold);
+        bool careful = j == 0 || !all_visible || !__all_sync(0xffffffffu, !ok || fabsf(m_used) <= kCoarseReference);
         if (!careful) {
           weights(kFirst, kMixed, p.scale_log2e, -m_used);
-          careful = __any_sync(0xffffffffu, !(m_new <= m_used + kRescaleThreshold));
+          careful = __any_sync(0xffffffffu, raised);
         }
         trace_event(trace, DYSPEC_TAG(1 + h, 3, j));
         if (!careful) {
@@ -525,7 +527,7 @@ causal_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         } else {
           if (j == 0) {
             m_used = m_new;
-          } else if (__any_sync(0xffffffffu, !(m_new <= m_used + kRescaleThreshold))) {
+          } else if (__any_sync(0xffffffffu, raised)) {
             // rescale the running output of this warp's 32 rows: O *= 2^(m_used - m_new)  (P V(j - 1) is done, see above)
             const float f = fast_exp2(m_used - (m_new == -INFINITY ? 0.f : m_new));
 #pragma unroll 1

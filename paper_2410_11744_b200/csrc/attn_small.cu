@@ -577,6 +577,10 @@ tree_attn_small_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
         const float z_lo = __shfl_xor_sync(0xffffffffu, mx_lo, 2), z_hi = __shfl_xor_sync(0xffffffffu, mx_hi, 2);
         mx_lo = fmaxf(mx_lo, z_lo) * p.scale_log2e; mx_hi = fmaxf(mx_hi, z_hi) * p.scale_log2e;
       }
+      if (kCausal) {                      // rows that are not the request's raise no reference: what their Q holds changes no bit of the others
+        if (!ok_lo) mx_lo = -INFINITY;
+        if (!ok_hi) mx_hi = -INFINITY;
+      }
       const float mn_lo = fmaxf(m_lo, mx_lo), mn_hi = fmaxf(m_hi, mx_hi);
       confirm_pv_done((got & 2u) != 0u);
       bool shifted = false;             // the scores are differences from the reference already

@@ -345,6 +345,21 @@ def test_repeated_calls_share_a_workspace_and_give_the_same_bits(B):
             assert torch.equal(c.out, want)
 
 
+def test_neighbouring_rows_change_no_bit(B):
+    """Rows of another request in the same tile of packed rows: whatever they hold, the request's own bits stay."""
+    import torch
+    for ns in ([3, 9, 5], [67, 70, 131], [131, 1, 90]):
+        p = Prompt(B, 8, 8, 2, 128, ns)
+        p.call()
+        torch.cuda.synchronize()
+        want = p.out[:ns[0]].clone()
+        for fill in (float("nan"), 300.0, 0.0):
+            p.q[ns[0]:] = fill
+            p.call()
+            torch.cuda.synchronize()
+            assert torch.equal(p.out[:ns[0]], want)
+
+
 def test_two_streams_with_workspaces_of_their_own(B):
     import torch
     a = Chunk(B, 3, 8, 2, 128, [5000, 50, 0], [200, 1, 300], 128)
