@@ -534,6 +534,10 @@ int dyspec_append_kv_paged(const dyspec_append_t* args, dyspec_stream_t stream);
  * dyspec_plan_create_prompt, dyspec_prompt_attention: whole prompts (c_r = 0) packed one behind the other, no cache: K and V
  * rows start at n_0 + ... + n_{r-1} too, with strides of their own (columns of one fused projection, say).
  *
+ * Workspace: one buffer, as large as the largest plan needs and zeroed once, may serve any number of chunk and prompt plans
+ * whose calls follow each other (a loop that plans every step, say).  Plans of trees keep their words elsewhere: do not let them
+ * use it in between.
+ *
  * Values: K and V of a sequence's own tokens must be finite.  (One that is not makes the rows behind it not finite, as the
  * formula says; V's also rows up to 255 tokens in front of it.)  Limits: c_r + n_r, and (sum n_r) * g, below 2^31 - 256.
  * The plans serve these calls only, and these calls take no other plans (DYSPEC_ERR_INVALID_ARG).

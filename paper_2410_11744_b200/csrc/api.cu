@@ -211,6 +211,7 @@ struct dyspec_plan {
   bool allow_queue = true;              // false: fixed lists only (callers that cannot provide zeroed queue words)
   size_t queue_offset = 0;              // dynamic plans: byte offset of the two queue words inside the caller's workspace
   size_t counters_offset = 0;           // plans with split groups: byte offset of the groups' counter pairs in the workspace
+  size_t partials_offset = 0;           // causal plans: byte offset of the partials (0: they come first)
   bool merge_last = false;              // causal plans, small tiles: a group's pieces are merged by the one that finishes last
   bool merge_in_kernel = false;         // tensor-core regime: split groups are merged by their own items, no combine launch
   int cluster_fit[9] = {-1, -1, -1, -1, -1, -1, -1, -1, -1};   // clusters of C CTAs of the regime's kernel the device holds at once (-1: not known)
@@ -1209,6 +1210,8 @@ int dyspec_append_kv_paged(const dyspec_append_t* args, dyspec_stream_t stream) 
   return e == cudaSuccess ? DYSPEC_OK : cuda_failed(e, "append launch");
 }
 
+constexpr size_t kControlBytes = 16384;   // causal plans: queue words, then two words for each of up to 2016 groups that the last piece merges
+
 // The part of planning behind the checks: regime, schedule, workspace.
 static void finish_host_plan(dyspec_plan* pl, int64_t max_rows) {
   // Regime: tcgen05 tiles (2 x 128 packed rows per item) when some request has more packed rows
@@ -1240,6 +1243,17 @@ static void finish_host_plan(dyspec_plan* pl, int64_t max_rows) {
     }
   }
   pl->workspace_bytes = size_t(pl->n_slots) * size_t(pl->bm) * (pl->d + 2) * sizeof(float);
+  if (pl->kind != PlanKind::kTree) {
+    // What has to be zero between calls, queue words and counters, lies at the same place in every causal plan's workspace, in
+    // front of the partials: a step's plan differs from the last step's, and one buffer serves them all.
+    if (pl->merge_last && kControlBytes - 256 < pl->split_groups.size() * 2 * sizeof(int32_t)) pl->merge_last = false;
+    pl->merge_in_kernel = pl->merge_last;
+    pl->queue_offset = 0;
+    pl->counters_offset = 256;
+    pl->partials_offset = kControlBytes;
+    if (pl->workspace_bytes > 0 || pl->dynamic) pl->workspace_bytes += kControlBytes;
+    return;
+  }
   if (pl->regime == 1 && pl->cluster > 1)   // cluster plan: the shares a CTA's peers cannot push into its shared memory
     pl->workspace_bytes = size_t(pl->n_ctas) * attn_tc_cluster_workspace_per_cta(pl->d, pl->cluster);
   if (!pl->split_groups.empty()) {      // the groups' counter pairs follow the partials
@@ -1247,7 +1261,7 @@ static void finish_host_plan(dyspec_plan* pl, int64_t max_rows) {
     pl->workspace_bytes = pl->counters_offset + ((pl->split_groups.size() * 2 * sizeof(int32_t) + 255) & ~size_t(255));
     // (the items of a group wait for each other inside the kernel: only when every CTA of the launch is
     //  resident at once, i.e. one CTA per SM and no more CTAs than SMs; a forced larger grid keeps the combine launch)
-    pl->merge_in_kernel = pl->merge_last || (pl->regime == 1 && pl->tune.combine_mode != 0 && pl->n_ctas <= pl->n_sms);
+    pl->merge_in_kernel = pl->regime == 1 && pl->tune.combine_mode != 0 && pl->n_ctas <= pl->n_sms;
   }
   if (pl->dynamic) {                    // the queue words follow the partials (there are none in such a plan today)
     pl->queue_offset = (pl->workspace_bytes + 255) & ~size_t(255);
@@ -1604,7 +1618,7 @@ static int run_attention(const dyspec_plan_t* plan, const void* q, const void* k
   p.reqs = plan->d_reqs; p.items = plan->d_items; p.groups = plan->d_groups;
   p.bits = ancestor_bits; p.out = static_cast<__nv_bfloat16*>(out);
   p.node_tiles = plan->tree_in_pages ? nullptr : node_tiles;   // the tile sets count unshifted tree tiles
-  p.partial = static_cast<float*>(workspace);
+  p.partial = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + plan->partials_offset);
   p.counters = plan->split_groups.empty() ? nullptr
                                           : reinterpret_cast<int32_t*>(static_cast<unsigned char*>(workspace) + plan->counters_offset);
   p.merge_in_kernel = plan->merge_in_kernel ? 1 : 0;

@@ -345,6 +345,22 @@ def test_repeated_calls_share_a_workspace_and_give_the_same_bits(B):
             assert torch.equal(c.out, want)
 
 
+def test_one_workspace_serves_the_plans_of_a_loop(B):
+    """Plans of different batches, which split, queue and merge differently, in turn over one buffer that was zeroed once."""
+    import torch
+    runs = [Chunk(B, 1, 8, 2, 128, [9000, 50, 0], [40, 1, 300], 128), Chunk(B, 2, 8, 1, 128, [12000, 50], [1, 1], 128),
+            Chunk(B, 3, 8, 2, 128, [700] * 30, [1] * 30, 128), Prompt(B, 4, 8, 8, 64, [900, 300, 2000]),
+            Chunk(B, 5, 8, 1, 128, [9001, 51], [1, 2], 128), Chunk(B, 6, 8, 2, 64, [20000], [9], 256), Prompt(B, 7, 4, 2, 128, [1, 3])]
+    ws = _zeros(max([256] + [c.plan.workspace_bytes() for c in runs]), dtype=torch.uint8)
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for c in runs:
+            c.out[:c.n] = 0
+            c.call(ws=ws)
+    for c in runs:
+        c.check()
+
+
 def test_neighbouring_rows_change_no_bit(B):
     """Rows of another request in the same tile of packed rows: whatever they hold, the request's own bits stay."""
     import torch
