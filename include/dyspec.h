@@ -539,7 +539,8 @@ int dyspec_append_kv_paged(const dyspec_append_t* args, dyspec_stream_t stream);
  * use it in between.
  *
  * Values: K and V of a sequence's own tokens must be finite.  (One that is not makes the rows behind it not finite, as the
- * formula says; V's also rows up to 255 tokens in front of it.)  Limits: c_r + n_r, and (sum n_r) * g, below 2^31 - 256.
+ * formula says; V's also rows up to 255 tokens in front of it.)  Limits: c_r + n_r, and (sum n_r) * g, below 2^31 - 256; at most
+ * 2^22 tiles of 64 packed rows (DYSPEC_ERR_UNSUPPORTED).
  * The plans serve these calls only, and these calls take no other plans (DYSPEC_ERR_INVALID_ARG).
  */
 int dyspec_plan_create_chunk(dyspec_plan_t** plan, int n_q_heads, int n_kv_heads, int head_dim, int n_req,

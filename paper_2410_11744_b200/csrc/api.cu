@@ -1376,6 +1376,7 @@ static int make_causal_plan(dyspec_plan_t** out, PlanKind kind, int n_q_heads, i
     max_rows = std::max(max_rows, n * g);
     groups += ((n * g + 63) / 64) * n_kv_heads;
   }
+  if (kind == PlanKind::kChunk && total > 0 && kv_total_rows == 0) return DYSPEC_ERR_INVALID_ARG;
   if (total * g >= (int64_t(1) << 31) - 256 || groups > (int64_t(1) << 22)) return DYSPEC_ERR_UNSUPPORTED;
   dyspec_plan* pl = nullptr;
   int rc = DYSPEC_OK;

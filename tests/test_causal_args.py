@@ -68,7 +68,7 @@ def test_plan_refusals(lib, chunk, code, over):
 
 @pytest.mark.parametrize("code,over", [
     (-1, dict(ctx=(-1,))), (-1, dict(ctx=None)), (-1, dict(page=0)), (-1, dict(page=192)), (-2, dict(page=64)), (-2, dict(page=1 << 21)),
-    (-1, dict(rows=-1)), (-2, dict(rows=1 << 31)), (-2, dict(ctx=(2 ** 31 - 300,), n=(100,))),
+    (-1, dict(rows=-1)), (-1, dict(rows=0)), (-2, dict(rows=1 << 31)), (-2, dict(ctx=(2 ** 31 - 300,), n=(100,))),
 ])
 def test_chunk_plan_refusals(lib, code, over):
     rc, h = _plan(lib, True, **over)
