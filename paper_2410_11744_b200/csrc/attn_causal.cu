@@ -28,8 +28,18 @@
 //   - 6 of 16 pairs of exponentials on the FMA pipe (4: 2 % slower; 0: 5 - 8 %; 8: 3 %).
 // Tried and slower: two threads per row (16 softmax warps, 104 registers: 130 - 138); one S buffer that the halves share, with P
 // beside it, as in the tree kernel (123); for D = 64, whose tensor memory has the room, P beside two S buffers (193 -> 221:
-// both softmaxes at once again); one issuer that asks for the next item's S before this one's output is out (long prompts + 3 %).
-// Neither half the loads (timing only) nor a finer ring changed anything.
+// both softmaxes at once again) or a third S buffer and an issuer that runs three products ahead, across items too (184 -> 223, the
+// same); one issuer that asks for the next item's S before this one's output is out (long prompts + 3 %).
+// Neither half the loads (timing only) nor a finer ring changed anything.  D = 64: 592 tokens over 15792 keys (64 / 8 heads) 181 - 194 us,
+// 2 440 cycles a tile, of which the softmax warps issue in 59 %, the exponential unit 52 %, the tensor pipe 41 %.
+//
+// An item costs about 4 us beside its tiles (a prompt of 700 tokens: a third of its time): masked tiles without the polynomial, the output,
+// and code that runs once per item and has to be fetched again (ncu: 0.73 cycles without an instruction per instruction issued, 0.24 on
+// long contexts).  Slower all the same: the next item's S in the turn of this one's last product, or without a turn (+ 3 - 20 %); the output
+// read in one go (+ 3 %); masked and first tiles 32 keys at a time in a loop from tensor memory, a quarter of the code (+ 6 % even on
+// long contexts: the fast path is scheduled differently); weights without a maximum, a tile's sum telling when the reference has to
+// rise (7 % fewer instructions, + 5 - 10 %); half B taking every other key tile of an item that has rows for half A only (batches of single
+// tokens with heads of 64 - 18 %, everything with two halves + 4 - 8 %).
 //
 // CTAs take items from a queue, longest first (see schedule_causal in api.cu); an item whose group was cut along the
 // keys writes an fp32 partial (O, m, l) that combine_kernel merges.  Every wait on an mbarrier is bounded (see mbar_wait_idle).
