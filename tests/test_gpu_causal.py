@@ -40,7 +40,7 @@ def _workspace(plan):
 class Chunk:
     """A batch of chunks over a pool whose rows that belong to nobody hold NaN, and whose pages are shuffled."""
 
-    def __init__(self, B, seed, hq, hkv, d, contexts, ns, page, q_scale=1.0, extra=3):
+    def __init__(self, B, seed, hq, hkv, d, contexts, ns, page, q_scale=1.0, extra=3, scale=0.0):
         import torch
         gen = torch.Generator(device="cuda")
         gen.manual_seed(seed)
@@ -60,7 +60,8 @@ class Chunk:
         self.q = _bf16(gen, self.n, hq, d, scale=q_scale)
         self.out = torch.full((self.n + extra, hq, d), 7.0, dtype=torch.bfloat16, device="cuda")
         self.table = torch.tensor(table, device="cuda")
-        self.plan = B.dyspec_plan_create_chunk(hq, hkv, d, contexts, ns, self.rows, page)
+        self.plan = B.dyspec_plan_create_chunk(hq, hkv, d, contexts, ns, self.rows, page, scale)
+        self.scale = scale if scale > 0 else None
         self.ws, self.status = _workspace(self.plan), _zeros(1, dtype=torch.int32)
 
     def call(self, **over):
@@ -83,7 +84,7 @@ class Chunk:
                 if n > sample:
                     rng = np.random.default_rng(r)
                     rows = sorted(set([0, 1, n - 2, n - 1] + [int(x) for x in rng.integers(0, n, sample)]))
-                want, bound = causal(self.q[at:at + n], self.k[self.seq_rows[r]], self.v[self.seq_rows[r]], c, rows=rows)
+                want, bound = causal(self.q[at:at + n], self.k[self.seq_rows[r]], self.v[self.seq_rows[r]], c, scale=self.scale, rows=rows)
                 got = out[at:at + n]
                 check(got if rows is None else got[rows], want, bound)
             at += n
@@ -158,6 +159,48 @@ def test_large_scores_and_growing_maxima(B):
         ramp = torch.linspace(0.05, 2.0, 1000 + n, device="cuda")
         c.k[c.seq_rows[0]] = (c.k[c.seq_rows[0]].float() * ramp[:, None, None]).to(torch.bfloat16)
         c.check_after_call()
+
+
+@pytest.mark.parametrize("scale", [0.01, 0.4, -1.0])
+def test_a_scale_of_the_callers(B, scale):
+    """Not 1 / sqrt(d); one that is not positive stands for that."""
+    Chunk(B, 9, 8, 2, 128, [700, 3], [1, 2], 128, scale=scale).check_after_call()
+    Chunk(B, 10, 8, 8, 64, [700, 0], [130, 70], 128, scale=scale).check_after_call()
+
+
+@pytest.mark.parametrize("hq,hkv,d", [(8, 2, 128), (4, 4, 64)])
+@pytest.mark.parametrize("n", [1, 200])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_scores_beyond_2_to_the_30(B, hq, hkv, d, n, sign):
+    """Scores of one product, sign * 2^40 * step(key): the softmax is 1 / ties on the keys of the largest one that a row sees.  Their weights
+    are exactly 1, so the output is the mean of their values but for P's rounding, the fp32 sum's and the output's."""
+    import torch
+    context = 500
+    c = Chunk(B, n, hq, hkv, d, [context], [n], 128)
+    step = (torch.arange(context + n, device="cuda") // 90 % 5 + 1).float()           # 1 .. 5, in runs of 90 keys
+    c.q[:], c.k[c.seq_rows[0]] = 0.0, 0.0
+    c.q[:, :, 3] = sign * 2.0 ** 40
+    c.k[c.seq_rows[0], :, 3] = step[:, None].to(torch.bfloat16)
+    c.call()
+    torch.cuda.synchronize()
+    assert int(c.status.item()) == 0
+    v = c.v[c.seq_rows[0]].double()
+    for i in {0, n // 2, n - 1}:
+        seen = sign * step[:context + i + 1]
+        ties = seen == seen.max()
+        for h in range(hq):
+            w = v[:context + i + 1][ties][:, h // (hq // hkv)]
+            want, size = w.mean(dim=0), w.abs().mean(dim=0)
+            bound = 2.0 ** -8 * (want.abs() + size) + 2.0 ** -15 * size + 2.0 ** -126
+            assert ((c.out[i, h].double() - want).abs() <= bound).all()
+
+
+def test_many_requests(B):
+    rng = np.random.default_rng(4)
+    ns = [int(x) for x in rng.integers(0, 3, 900)]
+    Chunk(B, 11, 4, 2, 64, [int(x) for x in rng.integers(0, 200, 900)], ns, 128).check_after_call()
+    ns[450] = 150                                                    # all of them on the tensor-core kernel
+    Chunk(B, 12, 4, 2, 64, [int(x) for x in rng.integers(0, 200, 900)], ns, 128).check_after_call()
 
 
 def test_strided_queries(B):
@@ -444,7 +487,7 @@ def test_plans_serve_their_own_calls_only(B):
         with pytest.raises(B.DyspecError) as e:
             call()
         assert e.value.code == -1
-    long = B.dyspec_plan_create_chunk(8, 1, 128, [30000], [64], 30720, 128)
+    long = B.dyspec_plan_create_chunk(8, 1, 128, [30000], [64], 30208, 128)
     assert long.workspace_bytes() > 256
     with pytest.raises(B.DyspecError) as e:
         B.dyspec_chunk_attention_paged(long, c.q, c.k, c.v, c.table, 300, c.out, ws[:256])
