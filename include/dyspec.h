@@ -196,7 +196,7 @@ int dyspec_plan_build_tree_mask(const dyspec_plan_t* plan, const int32_t* parent
  *   q              dev bf16 [sum n_r][H_q][D]            (16-byte aligned)
  *   k_cache,v_cache dev bf16 [kv_total_rows][H_kv][D]    (16-byte aligned)
  *   ancestor_bits  dev uint32 [sum n_r][W]               (from the mask builder)
- *   out            dev bf16 [sum n_r][H_q][D]            (written)
+ *   out            dev bf16 [sum n_r][H_q][D]            (written; 16-byte aligned)
  *   workspace      dev, >= dyspec_plan_workspace_bytes(plan), 256-byte aligned; it must be zero before the
  *                  first call (the caller zeroes it once; the kernels leave its counters zero).  Two
  *                  calls that overlap on the GPU need two workspaces (a workspace holds the split-KV
@@ -529,7 +529,7 @@ int dyspec_append_kv_paged(const dyspec_append_t* args, dyspec_stream_t stream);
  * c_r + n_r tokens; the same early read; a page number outside the pool reads as zeros).  Rows of a page behind the
  * sequence's last token are not used, whatever they hold.
  *   q    dev bf16, rows of n_q_heads * head_dim, q_stride values apart (0 = packed; a multiple of 8)
- *   out  dev bf16 [sum n_r][n_q_heads][head_dim] (written)
+ *   out  dev bf16 [sum n_r][n_q_heads][head_dim] (written; 16-byte aligned)
  *
  * dyspec_plan_create_prompt, dyspec_prompt_attention: whole prompts (c_r = 0) packed one behind the other, no cache: K and V
  * rows start at n_0 + ... + n_{r-1} too, with strides of their own (columns of one fused projection, say).

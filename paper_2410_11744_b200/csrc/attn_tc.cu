@@ -822,8 +822,7 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
 #pragma unroll
             for (int i = 0; i < 16; ++i)
               pk[i] = pack_bf16x2(__uint_as_float(v[2 * i]) * inv, __uint_as_float(v[2 * i + 1]) * inv);
-            st_global_v8(out + c * 32, pk);
-            st_global_v8(out + c * 32 + 16, pk + 8);
+            st_global_row16(out + c * 32, pk, wide_rows(p.out));
           }
         }
       } else {

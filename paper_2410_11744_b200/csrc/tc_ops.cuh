@@ -79,6 +79,19 @@ __device__ __forceinline__ void st_global_v8(void* ptr, const uint32_t* v) {
   asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
                ::"l"(ptr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
 }
+// 16 words of a row that is only known to be 16-byte aligned: 32-byte stores where `wide` (the same for the whole grid) says that the
+// row is 32-byte aligned, else 16-byte ones.
+__device__ __forceinline__ void st_global_row16(void* ptr, const uint32_t* v, bool wide) {
+  if (wide) {
+    st_global_v8(ptr, v);
+    st_global_v8(static_cast<uint32_t*>(ptr) + 8, v + 8);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) static_cast<uint4*>(ptr)[i] = make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+  }
+}
+// Output rows are multiples of 128 bytes, so the base decides; callers have to align it to 16 bytes.
+__device__ __forceinline__ bool wide_rows(const void* out) { return (reinterpret_cast<uintptr_t>(out) & 31) == 0; }
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
