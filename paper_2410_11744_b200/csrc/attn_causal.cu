@@ -25,7 +25,7 @@
 //   - Weights against the old reference beside the maximum, not behind it; P handed over in two pieces of 64 keys, so that
 //     the first half of P V runs under the second half of the weights (pieces of 32 + 96 or 96 + 32: 5 % slower).
 //   - An issuer per half, so that one's waits and commits run under the other's batch (2 - 3 %).
-//   - 6 of 16 pairs of exponentials on the FMA pipe (4: 2 % slower; 0: 5 - 8 %; 8: 3 %).
+//   - For heads of 64, 5 of 16 pairs of exponentials on the FMA pipe (see kPolyPairs).
 // Tried and slower: two threads per row (16 softmax warps, 104 registers: 130 - 138); one S buffer that the halves share, with P
 // beside it, as in the tree kernel (123); for D = 64, whose tensor memory has the room, P beside two S buffers (193 -> 221:
 // both softmaxes at once again) or a third S buffer and an issuer that runs three products ahead, across items too (184 -> 223, the
@@ -83,10 +83,10 @@ struct Bars {
   static constexpr int kCount = kItemEmpty + 8;
 };
 
-// 2^x for x <= 127 on the FMA pipe, two at a time: x = n + f with n the nearest integer, 2^f by the cubic with the smallest
-// largest relative error on [-1/2, 1/2] (7.5e-5, found by Remez exchange; P is rounded to bf16, 2^-9, right behind it), n
-// added to its exponent.  Below -125 the result stays at 2^-125 (relative to a row's largest term of 1, nothing); a NaN is
-// the caller's to keep away.
+// 2^x for x <= 127 on the FMA pipe, two at a time: x = n + f with n the nearest integer, 2^f by the quintic through 1 at f = 0 with the
+// smallest largest relative error on [-1/2, 1/2] (found as a linear program; 1.6e-7 as evaluated in fp32, the 2^-22 that the
+// exponential unit is held to is 2.4e-7), n added to its exponent.  Below -125 the result stays at 2^-125 (relative to a row's
+// largest term of 1, nothing); a NaN is the caller's to keep away.
 __device__ __forceinline__ uint64_t exp2_poly2(uint64_t x2) {
   constexpr float kMagic = 12582912.f;      // 1.5 * 2^23: adding it leaves the nearest integer in the low bits
   float x0, x1, t0, t1, p0, p1;
@@ -95,15 +95,22 @@ __device__ __forceinline__ uint64_t exp2_poly2(uint64_t x2) {
   const uint64_t t2 = add_f32x2(x2, pack_f32x2(kMagic, kMagic));
   const uint64_t n2 = add_f32x2(t2, pack_f32x2(-kMagic, -kMagic));
   const uint64_t f2 = fma_f32x2(n2, pack_f32x2(-1.f, -1.f), x2);
-  uint64_t p2 = fma_f32x2(pack_f32x2(0.0551716685f, 0.0551716685f), f2, pack_f32x2(0.242611125f, 0.242611125f));
-  p2 = fma_f32x2(p2, f2, pack_f32x2(0.693260968f, 0.693260968f));
-  p2 = fma_f32x2(p2, f2, pack_f32x2(0.999928057f, 0.999928057f));
+  auto both = [](float c) { return pack_f32x2(c, c); };
+  uint64_t p2 = fma_f32x2(both(0.00132647273f), f2, both(0.00967151299f));
+  p2 = fma_f32x2(p2, f2, both(0.0555073358f));
+  p2 = fma_f32x2(p2, f2, both(0.240222424f));
+  p2 = fma_f32x2(p2, f2, both(0.693147004f));
+  p2 = fma_f32x2(p2, f2, both(1.f));
   unpack_f32x2(t2, t0, t1);
   unpack_f32x2(p2, p0, p1);
   return pack_f32x2(__uint_as_float(__float_as_uint(p0) + (__float_as_uint(t0) << 23)),
                     __uint_as_float(__float_as_uint(p1) + (__float_as_uint(t1) << 23)));
 }
-constexpr int kPolyPairs = 6;             // of the 16 pairs in 32 keys, how many take the polynomial
+// Of the 16 pairs in 32 keys, how many take the polynomial.  Heads of 128 have products twice as long to hide the exponential unit under:
+// none (512 tokens over 8192 keys, 64 / 8 heads, cold: 124.0 us; 2 pairs 124.8, 5: 126.5).  Heads of 64 (592 tokens over 15200 keys, 64 / 8
+// heads): 202 us with 5 pairs, 208 - 214 with 0, 4, 6 or 7.  (A cubic, 7.5e-5, would give 196: not worth bits that the header promises.)
+template <int D>
+constexpr int kPolyPairs = D == 128 ? 0 : 5;
 __device__ __forceinline__ float max3_nan(float a, float b, float c) {
   float d;
   asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
@@ -520,7 +527,7 @@ causal_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         };
         constexpr std::integral_constant<int, 0> kFirst{}, kExact{};
         constexpr std::integral_constant<int, 1> kSecond{};
-        constexpr std::integral_constant<int, kPolyPairs> kMixed{};
+        constexpr std::integral_constant<int, kPolyPairs<D>> kMixed{};
         // The reference almost always stays: the first weights are computed against the one there is, beside the maximum
         // instead of behind it, and again in the rare tile that raises it.
         // (Rows that are not the request's have no vote: what their Q holds changes no bit of the others.)
