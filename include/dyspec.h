@@ -27,10 +27,18 @@
  *     inputs (parents, q, k_cache, v_cache, page_table: the attention kernels work through the prefix
  *     keys) before it waits for that kernel; everything it writes, and the mask and tile sets it reads,
  *     it touches only after the wait.  Inputs written by ordinary kernels or copies earlier in
- *     the stream are safe (without an early-launch signal the stream serialises fully, as always),
- *     and so is every sequence of this library's own calls.  The one thing to avoid is producing
- *     those inputs with a foreign kernel that itself signals early launch of its dependents
- *     (griddepcontrol.launch_dependents) directly before a call of this library.
+ *     the stream are safe (without an early-launch signal the stream serialises fully, as always).
+ *     This library's attention calls and mask builders signal early launch themselves, all its other
+ *     calls are ordinary kernels in this sense.  So two things are to be avoided, since the call would
+ *     read what is not written yet:
+ *       - `out` of an attention call (tree, chunk or prompt) as q, k, v or a cache of an attention call
+ *         behind it in the stream, with nothing but calls of attention and mask builders in between.  One
+ *         ordinary kernel or copy between the two is enough (a projection, cudaMemcpyAsync,
+ *         dyspec_append_kv_paged: what a model does with an attention's output);
+ *       - producing the inputs with a foreign kernel that itself signals early launch of its dependents
+ *         (griddepcontrol.launch_dependents) directly before a call of this library.
+ *     Every other sequence of this library's own calls is safe, one buffer as the output of many calls
+ *     or as input first and output later included.
  *
  * Packed rows: ancestor_bits[i][w], w < words_per_row, has bit b (LSB = bit 0) set iff tree node
  * 32*w + b is node i itself or an ancestor of node i (Sec. 2, the mask(A) equation, plus the self

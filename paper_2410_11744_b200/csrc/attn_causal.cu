@@ -423,8 +423,9 @@ causal_attn_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
     // ------------------------------------------------------------------ softmax + epilogue warps
-    // Q, K, V and the work items are inputs that no kernel launched with early start writes; only the output and the
-    // partials wait for the preceding kernels of the stream.
+    // The work items are written before the launch; Q, K, V and the page table are inputs that the kernels in front do not write when
+    // they signal early launch (no attention output without an ordinary kernel in between: the header's rule on stream
+    // order).  Only the output and the partials wait for the preceding kernels of the stream.
     bool dep_ok = false;
     const int h = (warp - 4) >> 2;                       // query half
     const int r = ((warp & 3) << 5) + lane;              // row of the half == TMEM lane

@@ -405,7 +405,8 @@ tree_attn_small_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_c
     if (p.cluster_size > 1) cluster_wait();
   } else {
   // -------------------------------------------------------------------- compute warps
-  // Work items and Q/K/V (through TMA) are inputs that no kernel launched with early start writes: the
+  // Work items and Q/K/V (through TMA) are inputs that the kernels in front do not write when they signal early
+  // launch (no attention output without an ordinary kernel in between: the header's rule on stream order): the
   // prefix tiles need nothing else, so they are processed while the preceding kernels of the stream may
   // still be running.  The mask, the partials and the output do depend on them: every thread waits
   // for the preceding kernels right before it first reads mask words or writes to global memory.

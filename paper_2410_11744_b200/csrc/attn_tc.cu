@@ -531,7 +531,8 @@ tree_attn_tc_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_cons
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
     // ------------------------------------------------------------------ softmax + epilogue warps
-    // Q/K/V and the work items are inputs no kernel launched with early start writes, and full prefix
+    // Q/K/V and the work items are inputs that the kernels in front do not write when they signal early launch (no
+    // attention output without an ordinary kernel in between: the header's rule on stream order), and full prefix
     // tiles need nothing else: they are processed while the preceding kernels of the stream may still be
     // running.  The mask, the tile sets, the partials and the output do depend on those kernels: the
     // thread waits for them right before it first touches any of these.
