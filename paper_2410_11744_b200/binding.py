@@ -394,6 +394,24 @@ def _host_i32(values: Sequence[int]):
     return (_c.c_int32 * max(1, len(values)))(*[int(x) for x in values])
 
 
+def _row_stride(t, call: str) -> int:
+    """Values from one token's row of a tensor to the next, 0 where they are packed (and for an address)."""
+    if t is None or isinstance(t, int) or t.is_contiguous():
+        return 0
+    if t.dim() > 1 and t.stride(0) > 0 and t[0].is_contiguous():      # columns of a fused projection, say
+        return t.stride(0)
+    raise DyspecError(-1, call)
+
+
+def _packed(t, call: str):
+    """The address of a tensor that the call takes without strides (a cache, a table, an output); other layouts are refused."""
+    if t is None or isinstance(t, int):
+        return t
+    if not t.is_contiguous():
+        raise DyspecError(-1, call)
+    return t.data_ptr()
+
+
 def dyspec_plan_create_chunk(n_q_heads: int, n_kv_heads: int, head_dim: int, context_len: Sequence[int], n_new: Sequence[int],
                              kv_total_rows: int, page_size: int, scale: float = 0.0) -> Plan:
     """Plan of causal attention of new tokens over a paged cache (see include/dyspec.h); lengths are host sequences."""
@@ -408,10 +426,12 @@ def dyspec_plan_create_chunk(n_q_heads: int, n_kv_heads: int, head_dim: int, con
 
 def dyspec_chunk_attention_paged(plan: Plan, q, k_cache, v_cache, page_table, pages_per_req: int, out, workspace=None,
                                  status=None, stream=None, q_stride: int = 0) -> None:
+    """Causal attention of the plan's chunks (see include/dyspec.h).  q_stride 0: q's own stride; caches and out are packed."""
+    call = "dyspec_chunk_attention_paged"
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(lib.dyspec_chunk_attention_paged(plan.handle, _ptr(q), q_stride, _ptr(k_cache), _ptr(v_cache), _ptr(page_table),
-                                            int(pages_per_req), _ptr(out), _ptr(workspace), ws_bytes, _ptr(status),
-                                            _stream(stream)), "dyspec_chunk_attention_paged")
+    _check(lib.dyspec_chunk_attention_paged(plan.handle, _ptr(q), q_stride or _row_stride(q, call), _packed(k_cache, call),
+                                            _packed(v_cache, call), _packed(page_table, call), int(pages_per_req), _packed(out, call),
+                                            _ptr(workspace), ws_bytes, _ptr(status), _stream(stream)), call)
 
 
 def dyspec_plan_create_prompt(n_q_heads: int, n_kv_heads: int, head_dim: int, seq_len: Sequence[int], scale: float = 0.0) -> Plan:
@@ -424,9 +444,12 @@ def dyspec_plan_create_prompt(n_q_heads: int, n_kv_heads: int, head_dim: int, se
 
 def dyspec_prompt_attention(plan: Plan, q, k, v, out, workspace=None, status=None, stream=None, q_stride: int = 0,
                             k_stride: int = 0, v_stride: int = 0) -> None:
+    """Causal attention of the plan's prompts (see include/dyspec.h).  Strides of 0: the tensors' own; out is packed."""
+    call = "dyspec_prompt_attention"
     ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(lib.dyspec_prompt_attention(plan.handle, _ptr(q), q_stride, _ptr(k), k_stride, _ptr(v), v_stride, _ptr(out),
-                                       _ptr(workspace), ws_bytes, _ptr(status), _stream(stream)), "dyspec_prompt_attention")
+    _check(lib.dyspec_prompt_attention(plan.handle, _ptr(q), q_stride or _row_stride(q, call), _ptr(k), k_stride or _row_stride(k, call),
+                                       _ptr(v), v_stride or _row_stride(v, call), _packed(out, call), _ptr(workspace), ws_bytes,
+                                       _ptr(status), _stream(stream)), call)
 
 
 # dyspec_append_t, packed by hand: ctypes takes 6 us to convert as many arguments one by one, more than the kernel of a decoding step
@@ -439,13 +462,15 @@ def dyspec_append_kv_paged(k_new, v_new, q, q_out, k_cache, v_cache, kv_total_ro
                            head_dim: int, k_stride: int = 0, v_stride: int = 0, q_stride: int = 0, q_out_stride: int = 0,
                            status=None, stream=None) -> None:
     """New tokens' K and V into the paged cache, K and Q rotated by position (see include/dyspec.h).  Strides count
-    values from one token's row to the next, 0 = packed; depths and tree_row_offset may be None."""
-    args = _APPEND_ARGS.pack(_ptr(k_new) or 0, _ptr(v_new) or 0, _ptr(q) or 0, _ptr(q_out) or 0, _ptr(k_cache) or 0, _ptr(v_cache) or 0,
-                             k_stride, v_stride, q_stride, q_out_stride, kv_total_rows, _ptr(token_offsets) or 0,
-                             _ptr(context_len) or 0, _ptr(depths) or 0, _ptr(tree_row_offset) or 0, _ptr(page_table) or 0,
-                             _ptr(rope_table) or 0, _ptr(status) or 0, n_req, n_tokens, n_q_heads, n_kv_heads, head_dim,
+    values from one token's row to the next, 0 = the tensor's own; depths and tree_row_offset may be None."""
+    call = "dyspec_append_kv_paged"
+    args = _APPEND_ARGS.pack(_ptr(k_new) or 0, _ptr(v_new) or 0, _ptr(q) or 0, _ptr(q_out) or 0, _packed(k_cache, call) or 0,
+                             _packed(v_cache, call) or 0, k_stride or _row_stride(k_new, call), v_stride or _row_stride(v_new, call),
+                             q_stride or _row_stride(q, call), q_out_stride or _row_stride(q_out, call), kv_total_rows, _ptr(token_offsets) or 0,
+                             _ptr(context_len) or 0, _ptr(depths) or 0, _ptr(tree_row_offset) or 0, _packed(page_table, call) or 0,
+                             _packed(rope_table, call) or 0, _ptr(status) or 0, n_req, n_tokens, n_q_heads, n_kv_heads, head_dim,
                              pages_per_req, page_size, n_positions, rotary_dim, interleaved)
-    _check(lib.dyspec_append_kv_paged(args, _stream(stream)), "dyspec_append_kv_paged")
+    _check(lib.dyspec_append_kv_paged(args, _stream(stream)), call)
 
 
 def dyspec_release_cache() -> None:
