@@ -90,7 +90,7 @@ __global__ void __launch_bounds__(kThreads, 4) append_kv_kernel(const AppendPara
   const int64_t tree0 = p.tree_row_offset ? __ldg(p.tree_row_offset + r) : 0;
   int64_t row = -1;
   if (p.tree_row_offset) {
-    row = tree0 < 0 ? -1 : tree0 + j;
+    row = tree0 < 0 || tree0 >= p.cache_rows ? -1 : tree0 + j;    // (no sum that could pass 63 bits)
   } else if (context >= 0) {
     const int64_t t = context + j, pi = t >> p.page_shift;
     const int page = pi < p.pages_per_req ? __ldg(p.page_table + int64_t(r) * p.pages_per_req + pi) : -1;
