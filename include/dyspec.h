@@ -179,8 +179,9 @@ int dyspec_set_tuning(int force_regime, int force_ctas, int combine_mode);
  * (per-CTA wall-clock stamps); in an ordinary build a non-NULL buffer is refused with
  * DYSPEC_ERR_UNSUPPORTED.  trace_buffer is a dev uint64 array of capacity_entries entries that the
  * caller zeroes; while set, CTA 0 of every tensor-core attention launch writes (tag << 44 | SM clock)
- * entries into three equal regions (MMA issuer, softmax half A, softmax half B; tags are listed in
- * csrc/attn_tc.cu; zero entries are unused).  When capacity_entries > 4096 the last 2048 entries are
+ * entries into equal regions, one per traced role: three for trees (MMA issuer, softmax half A, softmax half
+ * B; tags in csrc/attn_tc.cu), four for chunks and prompts (issuer A, softmax A, softmax B, issuer B; tags in
+ * csrc/attn_causal.cu); zero entries are unused.  When capacity_entries > 4096 the last 2048 entries are
  * not part of those regions: there each of the first 256 CTAs of an attention launch leaves 8
  * wall-clock stamps (globaltimer, ns) of its phases, listed where the kernels take them.  Pass
  * (NULL, 0) to switch it off (the default). */
@@ -209,8 +210,10 @@ int dyspec_plan_build_tree_mask(const dyspec_plan_t* plan, const int32_t* parent
  *                  first call (the caller zeroes it once; the kernels leave its counters zero).  Two
  *                  calls that overlap on the GPU need two workspaces (a workspace holds the split-KV
  *                  partials and words that a launch uses and clears: the arrival counters of the split
- *                  groups, the head of the plan's shared work queue); calls that follow each other on one stream may share one, and a
- *                  plan may be shared by any number of calls.
+ *                  groups, the head of the plan's shared work queue); calls that follow each other on one stream may share one
+ *                  when they use the same plan, or plans of the same batch structure: another plan's words lie
+ *                  elsewhere, and its partials may lie on this one's, so a buffer that passes from one structure to
+ *                  another is zeroed again in between.  A plan may be shared by any number of calls.
  *   status         dev int32 [1] or NULL
  */
 int dyspec_tree_attention_ragged(const dyspec_plan_t* plan, const void* q, const void* k_cache, const void* v_cache,
@@ -497,8 +500,9 @@ int dyspec_compact_kv_paged(void* k_cache, void* v_cache, const int64_t* tree_ro
  *   token_offsets    dev int32 [n_req + 1], from 0, not decreasing;  context_len dev int32 [n_req]
  *   n_tokens         rows of the inputs (host).  Rows from token_offsets[n_req] on belong to nobody and are left alone.
  *   depths           dev int32 [n_tokens] or NULL;  tree_row_offset dev int64 [n_req] or NULL
- *   page_table       dev int32 [n_req][pages_per_req]; page_size a power of two (any).  Not read with tree_row_offset
- *                    (NULL is fine then); else it holds a page for every new token.
+ *   page_table       dev int32 [n_req][pages_per_req]; page_size a power of two (any; the attention calls of this library
+ *                    read pages of 128 rows and more).  Not read with tree_row_offset (NULL is fine then); else it holds a page for
+ *                    every new token.
  *   rope_table       dev float [n_positions][rotary_dim], 16-byte aligned: cosines of the rotary_dim / 2 angles, then
  *                    their sines.  rotary_dim: a multiple of 16, at most head_dim (the columns behind it are copied);
  *                    0 = no rotation, rope_table NULL
@@ -536,15 +540,21 @@ int dyspec_append_kv_paged(const dyspec_append_t* args, dyspec_stream_t stream);
  * dyspec_chunk_attention_paged: page_table as in dyspec_tree_attention_paged with the tree rows inside the pages (it covers
  * c_r + n_r tokens; the same early read; a page number outside the pool reads as zeros).  Rows of a page behind the
  * sequence's last token are not used, whatever they hold.
- *   q    dev bf16, rows of n_q_heads * head_dim, q_stride values apart (0 = packed; a multiple of 8)
+ *   q    dev bf16, rows of n_q_heads * head_dim, q_stride values apart (0 = packed; a multiple of 8); 16-byte aligned like
+ *        K and V, and overlapped by out nowhere
  *   out  dev bf16 [sum n_r][n_q_heads][head_dim] (written; 16-byte aligned)
  *
  * dyspec_plan_create_prompt, dyspec_prompt_attention: whole prompts (c_r = 0) packed one behind the other, no cache: K and V
  * rows start at n_0 + ... + n_{r-1} too, with strides of their own (columns of one fused projection, say).
  *
+ * Lengths are the plan's: a step with other lengths takes a new plan (20 - 300 us of host time, shared by the layers of
+ * the step), and a captured graph of these calls serves the lengths that it was captured with.  (The append's lengths and
+ * contexts are device data: its graph serves any step of at most n_tokens tokens in
+ * n_req requests, empty ones among them.)
+ *
  * Workspace: one buffer, as large as the largest plan needs and zeroed once, may serve any number of chunk and prompt plans
- * whose calls follow each other (a loop that plans every step, say).  Plans of trees keep their words elsewhere: do not let them
- * use it in between.
+ * whose calls follow each other (a loop that plans every step, say).  Plans of trees keep their words elsewhere: a loop that
+ * also verifies trees gives them a workspace of their own.
  *
  * Values: K and V of a sequence's own tokens must be finite.  (One that is not makes the rows behind it not finite, as the
  * formula says; V's also rows up to 255 tokens in front of it.)  Limits: c_r + n_r, and (sum n_r) * g, below 2^31 - 256; at most

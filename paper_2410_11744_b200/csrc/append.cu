@@ -2,7 +2,7 @@
 // their queries rotated with them.  Token j of request r has position context[r] + j, or context[r] + depth[j]
 // when it is a node of a draft tree, and with half-split pairs (i, i + rot / 2), or neighbouring ones (2 i, 2 i + 1),
 //   (a, b) -> (a cos - b sin, b cos + a sin),   cos / sin = columns i and rot / 2 + i of the position's table row,
-// in fp32, rounded once to bf16 (half a step: 2^-9 relative to the larger of the pair).  V, and columns behind `rot`,
+// in fp32, rounded once to bf16 (half a step: 2^-8 relative).  V, and columns behind `rot`,
 // are copied bit for bit.
 //
 // Bound by bytes: every value is read once and written once.  The unit of work is 32 bytes of one head, the two
@@ -11,7 +11,7 @@
 // every head that it works on: its 16 cosines and sines stay in registers.  A thread asks for its chunks before it knows
 // where they go; the chain in front of the writes (request of the token, context, page) runs under those loads.
 // A token is worked on by a group of 32 to 256 threads, as many as leave each about kBatch units.  64 registers, four CTAs per
-// SM: 14891 tokens of 80 heads of 128 (618 MB) 94 us, 6.6 TB/s, against 100 with three CTAs of 80 registers.
+// SM: 14891 tokens of 80 heads of 128 (618 MB) 100.4 us call after call, 6.2 TB/s, against 102.6 with three CTAs of 80 registers.
 #include "common.cuh"
 
 namespace dyspec {

@@ -1,5 +1,5 @@
-// Causal attention of new tokens (a chunk of a sequence over its paged cache, or whole packed prompts), for requests whose
-// packed rows (tokens x GQA group) fill 128-row tiles:
+// Causal attention of new tokens (a chunk of a sequence over its paged cache, or whole packed prompts), for plans in which some
+// request has more than 64 packed rows (tokens x GQA group); all requests of such a plan are served here, single tokens too:
 //   out_i = sum_{t <= c + i} softmax_t(scale <q_i, k_t>) v_t          (token i of the chunk is token c + i of its sequence)
 //
 // One CTA per SM, 12 warps; a work item is 256 packed query rows of one (request, kv head), two halves A and B of 128, against
@@ -13,11 +13,12 @@
 // been read, and "S(j + 1) is there" also says that P V(j) is done: one barrier tells the softmax threads both, and the
 // running output may be rescaled then without another wait.
 //
-// What bounds it.  A tile is 2 048 cycles of the tensor pipe (D = 128, both halves), 2 048 of the exponential unit if it did all
-// exponentials, and about 1 200 issue slots of each scheduler; the chain of one half, S -> row -> weights -> P V -> next S, is
-// 3 000, of which the other half's products hide what they can.  Measured 3 150 - 3 300 cycles a tile: 512 tokens over 8192 keys
-// (64 / 8 heads of 128) 105 - 108 us warm, 1.3 PFLOP/s; a prompt of 16384 3.3 - 3.8 ms, 1.15 - 1.35 PFLOP/s, under the power cap.  What
-// it took, each measured against the step before on those 512 tokens:
+// What bounds it.  A tile is 2 048 cycles of the tensor pipe (D = 128, both halves), as many of the exponential unit, and about
+// 1 200 issue slots of each scheduler, but its period is the chain of one half, 3 320 cycles in a trace: S to registers 180, weights
+// 2 090, P V and the next S 1 050; the other half's products run beside it.  512 tokens over 8192 keys (64 / 8 heads of 128) take
+// 120 - 122 us with cold inputs, 1.17 PFLOP/s (101 - 116 over and over on the same inputs, by the clock that the power cap leaves); a prompt
+// of 16384 3.3 - 3.8 ms, 1.15 - 1.35 PFLOP/s, under the power cap.  What it took, each measured against the step before on those 512
+// tokens (on the same inputs):
 //   - Issuing in turns, A's P V and next S, then B's (153 -> 143 us).  Without turns both halves' products interleave, their S
 //     arrive together, both softmaxes run at once, and then the pipe waits for them: 4 430 cycles.
 //   - tcgen05.mma operands that the compiler knows to be uniform (elect.sync, values through a shuffle): 143 -> 122.  From ordinary
@@ -30,10 +31,10 @@
 // beside it, as in the tree kernel (123); for D = 64, whose tensor memory has the room, P beside two S buffers (193 -> 221:
 // both softmaxes at once again) or a third S buffer and an issuer that runs three products ahead, across items too (184 -> 223, the
 // same); one issuer that asks for the next item's S before this one's output is out (long prompts + 3 %).
-// Neither half the loads (timing only) nor a finer ring changed anything.  D = 64: 592 tokens over 15792 keys (64 / 8 heads) 181 - 194 us,
-// 2 440 cycles a tile, of which the softmax warps issue in 59 %, the exponential unit 52 %, the tensor pipe 41 %.
+// Neither half the loads (timing only) nor a finer ring changed anything.  D = 64: 592 tokens over 15792 keys (64 / 8 heads) 202 us, cold; a
+// scheduler issues in 57 % of the cycles, the exponential unit is busy in 54 %, the FMA pipe in 48, the tensor pipe in 39.
 //
-// An item costs about 4 us beside its tiles (a prompt of 700 tokens: a third of its time): masked tiles without the polynomial, the output,
+// An item costs about 4 us beside its tiles (a prompt of 700 tokens: a third of its time): masked tiles, the output,
 // and code that runs once per item and has to be fetched again (ncu: 0.73 cycles without an instruction per instruction issued, 0.24 on
 // long contexts).  Slower all the same: the next item's S in the turn of this one's last product, or without a turn (+ 3 - 20 %); the output
 // read in one go (+ 3 %); masked and first tiles 32 keys at a time in a loop from tensor memory, a quarter of the code (+ 6 % even on
@@ -107,8 +108,9 @@ __device__ __forceinline__ uint64_t exp2_poly2(uint64_t x2) {
                     __uint_as_float(__float_as_uint(p1) + (__float_as_uint(t1) << 23)));
 }
 // Of the 16 pairs in 32 keys, how many take the polynomial.  Heads of 128 have products twice as long to hide the exponential unit under:
-// none (512 tokens over 8192 keys, 64 / 8 heads, cold: 124.0 us; 2 pairs 124.8, 5: 126.5).  Heads of 64 (592 tokens over 15200 keys, 64 / 8
-// heads): 202 us with 5 pairs, 208 - 214 with 0, 4, 6 or 7.  (A cubic, 7.5e-5, would give 196: not worth bits that the header promises.)
+// none (512 tokens over 8192 keys, 64 / 8 heads, call after call: 121.4 us, 2 - 5 pairs 122.6 - 123.7; one call on an idle card, at the full
+// clock: 136.7, 4 pairs 134.2).  Heads of 64 (592 tokens over 15792 keys, 64 / 8 heads): 202 us with 5 pairs, 208 - 214 with 0, 4, 6 or 7.
+// (A cubic, 7.5e-5, would give 196, and heads of 128 131.5 on an idle card: not worth bits that the header promises.)
 template <int D>
 constexpr int kPolyPairs = D == 128 ? 0 : 5;
 __device__ __forceinline__ float max3_nan(float a, float b, float c) {
