@@ -1593,7 +1593,7 @@ static int run_attention(const dyspec_plan_t* plan, const void* q, const void* k
                          dyspec_stream_t stream, bool tables_in_stream, int64_t q_stride, int64_t k_stride, int64_t v_stride) {
   if (!plan) return DYSPEC_ERR_INVALID_ARG;
   const bool causal = plan->kind != PlanKind::kTree;       // no mask to read
-  if (!aligned(node_tiles, 4)) return DYSPEC_ERR_INVALID_ARG;
+  if (!aligned(node_tiles, 4) || !aligned(status, 4)) return DYSPEC_ERR_INVALID_ARG;
   if (plan->n_ctas == 0) return DYSPEC_OK;
   if (!q || !k_cache || !v_cache || (!ancestor_bits && !causal) || !out) return DYSPEC_ERR_INVALID_ARG;
   if (!aligned(q, 16) || !aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(out, 16) || !aligned(ancestor_bits, 16))
