@@ -150,7 +150,8 @@ int64_t dyspec_plan_info(const dyspec_plan_t* plan, int field);
  * packed query row, first key tile, one-past-last key tile, partial slot or -1, group id, number of
  * splits of the group), the per-CTA item ranges into cta_begin_out (host, n_ctas + 1 entries, at most
  * max_ctas) and, into info_out (host int64 [12]), dyspec_plan_info fields 0-7 followed by keys per
- * tile, workspace bytes, the cluster size and dyspec_plan_info field 10.  Any output pointer may be NULL.  Returns the item count or an error. */
+ * tile, workspace bytes (those of the partials and their words packed; dyspec_plan_workspace_bytes counts a fixed
+ * 16 KB for the words of a plan that needs any workspace), the cluster size and dyspec_plan_info field 10.  Any output pointer may be NULL.  Returns the item count or an error. */
 int dyspec_schedule_dry_run(int n_q_heads, int n_kv_heads, int head_dim, int n_req, const int32_t* prefix_len,
                             const int32_t* n_nodes, int words_per_row, int32_t* items_out, int max_items,
                             int32_t* cta_begin_out, int max_ctas, int64_t* info_out);
@@ -210,10 +211,9 @@ int dyspec_plan_build_tree_mask(const dyspec_plan_t* plan, const int32_t* parent
  *                  first call (the caller zeroes it once; the kernels leave its counters zero).  Two
  *                  calls that overlap on the GPU need two workspaces (a workspace holds the split-KV
  *                  partials and words that a launch uses and clears: the arrival counters of the split
- *                  groups, the head of the plan's shared work queue); calls that follow each other on one stream may share one
- *                  when they use the same plan, or plans of the same batch structure: another plan's words lie
- *                  elsewhere, and its partials may lie on this one's, so a buffer that passes from one structure to
- *                  another is zeroed again in between.  A plan may be shared by any number of calls.
+ *                  groups, the head of the plan's shared work queue); calls that follow each other on one stream may share
+ *                  one, whatever their plans (trees, chunks, prompts): as large as the largest needs, zeroed once.  A plan may
+ *                  be shared by any number of calls.
  *   status         dev int32 [1] or NULL
  */
 int dyspec_tree_attention_ragged(const dyspec_plan_t* plan, const void* q, const void* k_cache, const void* v_cache,
@@ -552,9 +552,7 @@ int dyspec_append_kv_paged(const dyspec_append_t* args, dyspec_stream_t stream);
  * contexts are device data: its graph serves any step of at most n_tokens tokens in
  * n_req requests, empty ones among them.)
  *
- * Workspace: one buffer, as large as the largest plan needs and zeroed once, may serve any number of chunk and prompt plans
- * whose calls follow each other (a loop that plans every step, say).  Plans of trees keep their words elsewhere: a loop that
- * also verifies trees gives them a workspace of their own.
+ * Workspace: as in (3); one buffer serves all plans of a loop that plans every step, those of its trees among them.
  *
  * Values: K and V of a sequence's own tokens must be finite.  (One that is not makes the rows behind it not finite, as the
  * formula says; V's also rows up to 255 tokens in front of it.)  Limits: c_r + n_r, and (sum n_r) * g, below 2^31 - 256; at most

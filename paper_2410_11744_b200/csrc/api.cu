@@ -211,7 +211,7 @@ struct dyspec_plan {
   bool allow_queue = true;              // false: fixed lists only (callers that cannot provide zeroed queue words)
   size_t queue_offset = 0;              // dynamic plans: byte offset of the two queue words inside the caller's workspace
   size_t counters_offset = 0;           // plans with split groups: byte offset of the groups' counter pairs in the workspace
-  size_t partials_offset = 0;           // causal plans: byte offset of the partials (0: they come first)
+  size_t partials_offset = 0;           // byte offset of the partials in the workspace
   bool merge_last = false;              // causal plans, small tiles: a group's pieces are merged by the one that finishes last
   bool merge_in_kernel = false;         // tensor-core regime: split groups are merged by their own items, no combine launch
   int cluster_fit[9] = {-1, -1, -1, -1, -1, -1, -1, -1, -1};   // clusters of C CTAs of the regime's kernel the device holds at once (-1: not known)
@@ -1210,7 +1210,25 @@ int dyspec_append_kv_paged(const dyspec_append_t* args, dyspec_stream_t stream) 
   return e == cudaSuccess ? DYSPEC_OK : cuda_failed(e, "append launch");
 }
 
-constexpr size_t kControlBytes = 16384;   // causal plans: queue words, then two words for each of up to 2016 groups that the last piece merges
+// Bytes of a plan's partials: of split groups, or the shares that the CTAs of a tensor-core cluster plan pass to their peers.
+static size_t partial_bytes(const dyspec_plan& pl) {
+  if (pl.regime == 1 && pl.cluster > 1) return size_t(pl.n_ctas) * attn_tc_cluster_workspace_per_cta(pl.d, pl.cluster);
+  return size_t(pl.n_slots) * size_t(pl.bm) * size_t(pl.d + 2) * sizeof(float);
+}
+
+// Workspace of a plan that belongs to the caller.  What has to be zero between calls, queue words and counter pairs, lies at the same
+// place in every plan's workspace, in front of the partials: a step's plan differs from the last step's, and one buffer,
+// zeroed once, serves them all, trees, chunks and prompts.  256 bytes for the queue's words, then the counter pairs of up to 2016
+// split groups; with more of them the combine launch merges.
+constexpr size_t kControlBytes = 16384;
+static void place_control_words(dyspec_plan* pl) {
+  if (kControlBytes - 256 < pl->split_groups.size() * 2 * sizeof(int32_t)) pl->merge_in_kernel = false;
+  pl->queue_offset = 0;
+  pl->counters_offset = 256;
+  pl->partials_offset = kControlBytes;
+  pl->workspace_bytes = partial_bytes(*pl);
+  if (pl->workspace_bytes > 0 || pl->dynamic) pl->workspace_bytes += kControlBytes;
+}
 
 // The part of planning behind the checks: regime, schedule, workspace.
 static void finish_host_plan(dyspec_plan* pl, int64_t max_rows) {
@@ -1242,20 +1260,14 @@ static void finish_host_plan(dyspec_plan* pl, int64_t max_rows) {
       schedule(*pl);
     }
   }
-  pl->workspace_bytes = size_t(pl->n_slots) * size_t(pl->bm) * (pl->d + 2) * sizeof(float);
   if (pl->kind != PlanKind::kTree) {
-    // What has to be zero between calls, queue words and counters, lies at the same place in every causal plan's workspace, in
-    // front of the partials: a step's plan differs from the last step's, and one buffer serves them all.
-    if (pl->merge_last && kControlBytes - 256 < pl->split_groups.size() * 2 * sizeof(int32_t)) pl->merge_last = false;
     pl->merge_in_kernel = pl->merge_last;
-    pl->queue_offset = 0;
-    pl->counters_offset = 256;
-    pl->partials_offset = kControlBytes;
-    if (pl->workspace_bytes > 0 || pl->dynamic) pl->workspace_bytes += kControlBytes;
+    place_control_words(pl);
     return;
   }
-  if (pl->regime == 1 && pl->cluster > 1)   // cluster plan: the shares a CTA's peers cannot push into its shared memory
-    pl->workspace_bytes = size_t(pl->n_ctas) * attn_tc_cluster_workspace_per_cta(pl->d, pl->cluster);
+  // Trees: the words behind the partials, which is what a plan takes whose workspace is the library's own (single requests,
+  // the static form, the dry run); the plans that callers get are laid out by place_control_words.
+  pl->workspace_bytes = partial_bytes(*pl);
   if (!pl->split_groups.empty()) {      // the groups' counter pairs follow the partials
     pl->counters_offset = (pl->workspace_bytes + 255) & ~size_t(255);
     pl->workspace_bytes = pl->counters_offset + ((pl->split_groups.size() * 2 * sizeof(int32_t) + 255) & ~size_t(255));
@@ -1327,6 +1339,7 @@ int dyspec_plan_create(dyspec_plan_t** plan, int n_q_heads, int n_kv_heads, int 
                           kv_total_rows, words_per_row, scale);
   *plan = nullptr;
   if (rc != DYSPEC_OK) return rc;
+  place_control_words(pl);
   rc = upload(*pl);
   if (rc != DYSPEC_OK) { dyspec_plan_destroy(pl); return rc; }
   *plan = pl;
@@ -1346,6 +1359,7 @@ int dyspec_plan_create_paged(dyspec_plan_t** plan, int n_q_heads, int n_kv_heads
   int rc = make_host_plan(&pl, n_q_heads, n_kv_heads, head_dim, n_req, prefix_len, n_nodes,
                           in_pages ? zeros.data() : tree_row_offset, kv_total_rows, words_per_row, scale, page_size, true, in_pages);
   if (rc != DYSPEC_OK) return rc;
+  place_control_words(pl);
   rc = upload(*pl);
   if (rc != DYSPEC_OK) { dyspec_plan_destroy(pl); return rc; }
   *plan = pl;
